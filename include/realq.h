@@ -140,7 +140,8 @@ const char* realq_last_error(const realq_ctx* ctx);
  * Gram form), "dense_loss" (final loss with a dense metric), "saliency", "block_init" and
  * "block_step" (the block sweeps: the fixed forwards, one Block-GD step) and "attention"
  * (realq_decoder_block_sweep: each attention forward or backward with its rotary embeddings),
- * "metric" (the dense-metric product of a Block-GD step).
+ * "metric" (the dense-metric product of a Block-GD step), "logprobs", "packed_attention" and
+ * "linear_i8" (one entry per call of those operators).
  * Returns REALQ_ERR_INVALID_ARG for an unknown name.  Independently of this switch, each of
  * these phases (and each column block of realq_quantize_layer) is a roctx range of the same
  * name around its launches, visible with `rocprofv3 --marker-trace`. */
@@ -537,6 +538,118 @@ typedef struct realq_decoder_fwd_out {
 } realq_decoder_fwd_out;
 
 int realq_decoder_forward(realq_ctx* ctx, const realq_decoder_desc* desc, realq_decoder_fwd_out* out);
+
+/* ------------------------------------------------------------------ running, scoring and differentiating a model
+ * Stage 0 (Alg. 1) starts from the loss of the calibration tokens and its gradient at the logits,
+ * passes it back through attention over prompts of different lengths, and a quantized model is run
+ * and scored with the same operators.  They take their scratch memory from the caller, so that a
+ * captured graph keeps its own, allocate nothing, synchronise nothing and run on the context's
+ * device whichever is current.  dtype arguments: */
+#define REALQ_BF16 0
+#define REALQ_F32 1
+
+/* Log probabilities of given tokens.  For every row z of logits ([T, V], rows ld elements apart,
+ * ld >= V, bf16 or float32), in float32 throughout:
+ *   lse      = log sum_j e^z_j                                     [T], required
+ *   logp     = z_y - lse for the row's target y                    [T] | NULL (needs targets)
+ *   entropy  = -sum_j p_j log p_j,  p_j = e^(z_j - lse)            [T] | NULL
+ *   top_ids, top_logp: the `top` largest logits' columns and log probabilities, larger first, equal
+ *              logits (-0 equals 0) by the lower column            [T, top], required when top > 0
+ * Masked tokens carry -infinity (p = 0; as alternatives they come last, with log probability
+ * -infinity).  A row with nothing but -infinity has lse and log probabilities -infinity and
+ * entropy 0.  A row with a NaN or +infinity has NaN results (its top_ids stay in 0 .. V-1).  A
+ * target below 0 stands for no token: logp is 0.  A target of V or more reads nothing: logp is NaN.
+ * 1 <= V < 2^31, 0 <= top <= min(V, REALQ_LOGPROBS_MAX_TOP); T == 0 is a no-op.  work: scratch
+ * memory of at least realq_token_logprobs_workspace bytes, aligned to 16 (NULL when that is 0);
+ * its size depends on T, V, top, dtype and the device, its contents need no clearing and are not
+ * kept.
+ *
+ * realq_token_logprobs_backward: the gradient at the logits ([T, V], rows ldd apart, the logits'
+ * type; it may be the logits themselves with ldd = ld, not overlap them otherwise) of a loss with
+ * the given derivatives with respect to logp [T], entropy [T] and top_logp [T, top] (each may be NULL):
+ *   dz_j = -p_j (c + dentropy (log p_j + entropy)) + [j = y] dlogp + sum_k [j = top_ids_k] dtop_k,
+ *   c = dlogp + sum_k dtop_k,
+ * rounded once.  lse, entropy and top_ids as the forward call gave them (entropy only with
+ * dentropy, top_ids only with dtop; a column listed more than once receives the sum, one outside
+ * 0 .. V-1 nothing).  A target below 0 takes no part; one of V or more makes its row NaN where
+ * dlogp is given; an empty row's gradient is 0. */
+#define REALQ_LOGPROBS_MAX_TOP 64
+typedef struct realq_logprobs_desc {
+    int64_t T, V, ld;
+    const void* logits;       /* [T, ld]                                        */
+    const int64_t* targets;   /* [T] | NULL                                     */
+    int32_t dtype;            /* of the logits                                  */
+    int32_t top;
+} realq_logprobs_desc;
+
+int realq_token_logprobs_workspace(realq_ctx* ctx, const realq_logprobs_desc* desc, size_t* bytes);
+int realq_token_logprobs(realq_ctx* ctx, const realq_logprobs_desc* desc, float* logp, float* lse, float* entropy,
+                         int64_t* top_ids, float* top_logp, void* work, size_t work_bytes);
+int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* desc, const float* lse,
+                                  const float* entropy, const int64_t* top_ids, const float* dlogp,
+                                  const float* dentropy, const float* dtop, void* dlogits, int64_t ldd);
+
+/* Causal attention over packed sequences of any lengths (the attention of realq_decoder_forward,
+ * which takes equal sequences, without its rotary embedding).  q: [T, n_heads head_dim], k and v:
+ * [T, n_kv head_dim] bf16, token-major, rows ldq / ldk / ldv elements apart; query head h reads
+ * key/value head h / (n_heads / n_kv).  Sequence b holds rows cu_seqlens[b] .. cu_seqlens[b+1] - 1
+ * (device array of n_seqs + 1 non-decreasing offsets within 0 .. T; a sequence may be empty); token
+ * i of a sequence sees its tokens 0 .. i:
+ *   O_i = sum_j P_ij v_j,  P_ij = e^(scale q_i k_j - lse_i),  lse_i = log sum_j e^(scale q_i k_j)
+ * O: [T, n_heads head_dim] bf16, rows ldo apart; lse: [n_heads, T] float32 | NULL (the backward
+ * needs it).  Rows outside every sequence are left as they were.  scale 0 means 1 / sqrt(head_dim).
+ * Products of bf16 operands with float32 sums; softmax statistics in float32; the probabilities
+ * (and dS in the backward) are rounded to bf16 as operands.
+ *
+ * realq_packed_attention_backward: from dO, dQ (like q), dK and dV (like k, v; summed over the query
+ * heads that share them), rows lddq / lddk / lddv apart, bf16, by the formulas
+ *   dV = P^T dO,  dS = P (dO v^T - delta),  delta_i = sum O_i dO_i,  dQ = scale dS k,  dK = scale dS^T q;
+ * O and lse as the forward call gave them; delta: [n_heads, T] float32 scratch.  The sums have a
+ * fixed order: the same inputs give the same bits.  Outputs must not overlap inputs or each other
+ * (rows of one wider array are fine).
+ *
+ * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
+ * 128, 256); every array on 16 bytes and every row stride a multiple of 8.  q, k, v and dO must be
+ * finite: a NaN or an infinity can reach every row of its own sequence, and no other sequence.  Offsets that
+ * decrease or leave 0 .. T are cut to the arrays, with results of no meaning. */
+typedef struct realq_attention_desc {
+    int64_t T, n_seqs;
+    int32_t n_heads, n_kv, head_dim;
+    float scale;
+    const int32_t* cu_seqlens;  /* [n_seqs + 1]                                  */
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    int64_t ldq, ldk, ldv;
+} realq_attention_desc;
+
+int realq_packed_attention(realq_ctx* ctx, const realq_attention_desc* desc, uint16_t* O, int64_t ldo, float* lse);
+int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* desc, const uint16_t* O, int64_t ldo,
+                                    const float* lse, const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ,
+                                    int64_t lddq, uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv);
+
+/* Product in 8-bit integers with a scale per token and per output channel: the hand-off of a module
+ * quantized per row (realq_qparams.group = 0; its weights are codes - zeros with one scale per
+ * row), on activations rounded to 8 bits per token.
+ *
+ * realq_quantize_rows_i8: for each row x of X ([T, n] bf16 or float32, rows ldx apart)
+ *   scale = float32(max_j |x_j| / 127),  Q_j = x_j / scale rounded to the nearest whole number, ties to
+ *   even, cut to -127 .. 127 (the quotient's exact value decides, not its float32 rounding)
+ * Q: [T, n] int8, rows ldq apart; scale: [T].  A row of zeros has scale 0 and codes 0; a row with a
+ * NaN or an infinity has scale NaN and codes 0, so products with it are NaN.  Weights [m, n] can be
+ * quantized by the same call.
+ *
+ * realq_linear_i8: Y[t, i] = sx_t sw_i sum_j X[t, j] W[i, j] (+ bias_i), rounded once to dtype from
+ * float32.  X: [T, n] int8 rows ldx apart, W: [m, n] int8 rows ldw apart, sx: [T], sw: [m],
+ * bias: [m] float32 | NULL, Y: [T, m] rows ldy apart.  The sums are exact (32-bit integers), so
+ * n <= REALQ_I8_MAX_COLUMNS.  X and W on 16 bytes with row strides that are multiples of 16 run
+ * fastest; others take a path that assembles them byte by byte.  T == 0 is a no-op in both. */
+#define REALQ_I8_MAX_COLUMNS 131071
+int realq_quantize_rows_i8(realq_ctx* ctx, const void* X, int32_t dtype, int64_t T, int64_t n, int64_t ldx, int8_t* Q,
+                           int64_t ldq, float* scale);
+int realq_linear_i8(realq_ctx* ctx, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W, int64_t ldw,
+                    const float* sw, const float* bias, int64_t T, int64_t n, int64_t m, void* Y, int32_t dtype,
+                    int64_t ldy);
 
 #ifdef __cplusplus
 }

@@ -215,7 +215,8 @@ int realq_ctx_set_timing(realq_ctx* ctx, int enable) {
 static const char* kTimedNames[] = {"hessian",    "chol",      "quantize",   "obs",        "lock",
                                     "resid",      "grad",      "resid_inc",  "grad_inc",   "adam",
                                     "init",       "gram",      "gram_step",  "dense_loss", "saliency",
-                                    "block_init", "block_step", "attention", "metric"};
+                                    "block_init", "block_step", "attention", "metric",     "logprobs",
+                                    "packed_attention", "linear_i8"};
 
 int realq_ctx_kernel_time(realq_ctx* ctx, const char* name, int64_t* launches, double* total_ms) {
     if (!ctx || !name) return REALQ_ERR_INVALID_ARG;

@@ -1,0 +1,410 @@
+// Causal attention over packed sequences with grouped key/value heads, forward and backward
+// (realq_packed_attention, realq_packed_attention_backward).
+//
+//   S_ij = scale q_i k_j (j <= i, same sequence),  P = softmax_j S,  O = P v,  lse_i = log sum_j e^S_ij
+//   dV = P^T dO,  dP = dO V^T,  delta_i = sum dO_i O_i,  dS = P (dP - delta),
+//   dQ = scale dS K,  dK = scale dS^T Q   (dK, dV summed over the query heads of a key/value head)
+//
+// All products run on v_mfma_f32_32x32x16_bf16 with float32 sums.  Each product is arranged so that its
+// 32 x 32 result leaves the matrix unit in the layout in which the next product takes it as an operand:
+// a lane holds one column, its 16 registers rows 8 (e / 4) + 4 (lane / 32) + e % 4, and the next
+// product's contraction index simply runs in that order, with the other operand read from LDS in the same
+// order by transposing reads (ds_read_b64_tr_b16).  So P and dS stay in registers; they are rounded to
+// bf16 as operands (at most 2^-9 of each entry, on sums of many), while maxima, exponents, row sums,
+// delta and all accumulators are float32.
+//
+// LDS tiles hold rows of HD channels in 16-byte chunks, chunk c of row r at c ^ f(r): 16 consecutive rows
+// read at one chunk, and 4 rows read at 4 chunks, each fall on distinct banks.
+#include "common.h"
+#include "kernels.h"
+
+namespace realq {
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <int HD>
+__device__ __forceinline__ int swz(int r) {
+    if constexpr (HD == 64) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    else return ((r & 3) << 2) | ((r >> 2) & 3);
+}
+template <int HD>
+__device__ __forceinline__ int place(int r, int c) {  // uint16 index of chunk c of row r
+    return r * HD + ((c ^ swz<HD>(r)) << 3);
+}
+
+// Operand with the row (or column) in lane % 32 and channels 16 s + 8 (lane / 32) .. + 7.
+template <int HD>
+__device__ __forceinline__ bf16x8 row_frag(const uint16_t* lds, int row0, int s, int lane) {
+    return __builtin_bit_cast(
+        bf16x8, *reinterpret_cast<const u16x8*>(lds + place<HD>(row0 + (lane & 31), 2 * s + (lane >> 5))));
+}
+// Operand with channel 32 t + lane % 32 in the lane and the 16 rows from row0 on as contraction index, in
+// the order a 32 x 32 result holds them: 4 (lane / 32) + 0..3, then 8 more.
+template <int HD>
+__device__ __forceinline__ bf16x8 col_frag(const uint16_t* lds, int row0, int t, int lane) {
+    const int g = lane >> 4, i = lane & 15;  // a group of 16 lanes reads 4 rows of 16 channels
+    const int r = row0 + 4 * (g >> 1) + (i >> 2);
+    const int ch = 32 * t + 16 * (g & 1) + 4 * (i & 3);
+    auto rd = [&](int row) {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds + place<HD>(row, ch >> 3) + (ch & 7)));
+    };
+    struct {
+        s16x4 a, b;
+    } v = {rd(r), rd(r + 8)};
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const f32x2 x = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+// Registers 8 h .. 8 h + 7 of a result as the operand of the next product.
+__device__ __forceinline__ bf16x8 pack_frag(const f32x16& p, int h) {
+    const u32x4 v = {pack2(p[8 * h], p[8 * h + 1]), pack2(p[8 * h + 2], p[8 * h + 3]),
+                     pack2(p[8 * h + 4], p[8 * h + 5]), pack2(p[8 * h + 6], p[8 * h + 7])};
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ float other_half(float x) {
+    return __int_as_float(__builtin_amdgcn_ds_bpermute(((threadIdx.x & 63) ^ 32) << 2, __float_as_int(x)));
+}
+__device__ __forceinline__ f32x16 zero16() {
+    f32x16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e] = 0.f;
+    return z;
+}
+// Row of register e of a result, in this lane.
+__device__ __forceinline__ int crow(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
+
+struct Seq {
+    int64_t begin;  // first row
+    int len;        // rows
+    int tile;       // this block's tile
+    bool any;
+};
+// Tiles are dealt over the rows: sequence b owns the slots cu[b] / BM + b on, at least as many as it
+// has tiles of BM rows, so a slot is found without the lengths on the host.  Offsets are cut to 0..T:
+// whatever they hold, a block stays inside the arrays.
+template <int BM>
+__device__ __forceinline__ Seq find_tile(const int32_t* __restrict__ cu, int64_t n_seqs, int64_t T, int64_t slot) {
+    const int lane = threadIdx.x & 63;
+    auto at = [&](int64_t b) { return min(max((int64_t)cu[b], (int64_t)0), T); };
+    int64_t lo = 0, count = n_seqs;  // the sequence is among lo .. lo + count - 1
+    while (count > 1) {
+        const int64_t step = (count + 63) / 64;
+        const int64_t b = lo + lane * step;
+        const bool starts = lane * step < count && at(b) / BM + b <= slot;
+        const uint64_t v = __ballot(starts);
+        const int64_t k = v ? 63 - __builtin_clzll(v) : 0;
+        lo += k * step;
+        count = min(step, count - k * step);
+    }
+    Seq s;
+    s.begin = at(lo);
+    s.len = (int)max(at(lo + 1) - s.begin, (int64_t)0);
+    const int64_t j = slot - (s.begin / BM + lo);
+    s.any = j >= 0 && j * BM < s.len;
+    s.tile = s.any ? (int)j : 0;
+    return s;
+}
+
+// rows r0 .. r0 + ROWS - 1 (past the last one: the last one again) of one head into an LDS tile
+template <int HD, int ROWS, int NT>
+__device__ __forceinline__ void stage(const uint16_t* __restrict__ g, int64_t ld, int hd, int r0, int len,
+                                      uint16_t* lds) {
+    constexpr int CH = HD / 8;
+#pragma unroll
+    for (int c = 0; c < ROWS * CH / NT; ++c) {
+        const int i = threadIdx.x + c * NT, r = i / CH, ch = i % CH;
+        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (ch * 8 < hd) v = *reinterpret_cast<const u16x8*>(g + (int64_t)min(r0 + r, len - 1) * ld + ch * 8);
+        *reinterpret_cast<u16x8*>(lds + place<HD>(r, ch)) = v;
+    }
+}
+// row `row` of one head as an operand held in registers
+template <int HD>
+__device__ __forceinline__ void hold(const uint16_t* __restrict__ g, int hd, int lane, bf16x8 (&f)[HD / 16]) {
+#pragma unroll
+    for (int s = 0; s < HD / 16; ++s) {
+        const int ch = 16 * s + 8 * (lane >> 5);
+        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (ch < hd) v = *reinterpret_cast<const u16x8*>(g + ch);
+        f[s] = __builtin_bit_cast(bf16x8, v);
+    }
+}
+
+constexpr int NT = 256, BM = 128;
+
+}  // namespace
+
+template <int HD>
+__global__ __launch_bounds__(NT) void attn_forward_kernel(AttnArgs a, uint16_t* __restrict__ O, int64_t ldo,
+                                                          float* __restrict__ lse) {
+    constexpr int BN = 64;
+    __shared__ __attribute__((aligned(16))) uint16_t sk[BN * HD], sv[BN * HD];
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+    if (!sq.any) return;
+    const int h = blockIdx.y, kv = h / (a.n_heads / a.n_kv);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int q0 = sq.tile * BM + wave * 32;          // this wave's first query, in the sequence
+    const int qi = min(q0 + (lane & 31), sq.len - 1);  // this lane's
+    const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
+    const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
+    bf16x8 qf[HD / 16];
+    hold<HD>(a.q + (sq.begin + qi) * a.ldq + h * a.hd, a.hd, lane, qf);
+    const float c = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.f;
+    f32x16 o[HD / 32];
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t) o[t] = zero16();
+    const int keys = min((sq.tile + 1) * BM, sq.len);
+    for (int k0 = 0; k0 < keys; k0 += BN) {
+        __syncthreads();
+        stage<HD, BN, NT>(K, a.ldk, a.hd, k0, sq.len, sk);
+        stage<HD, BN, NT>(V, a.ldv, a.hd, k0, sq.len, sv);
+        __syncthreads();
+        if (k0 > q0 + 31) continue;
+        f32x16 s[2] = {zero16(), zero16()};
+#pragma unroll
+        for (int u = 0; u < HD / 16; ++u)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) s[b] = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s[b]);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if (k0 + 32 * b + crow(e, lane) > qi) s[b][e] = -INFINITY;
+                mx = fmaxf(mx, s[b][e]);
+            }
+        mx = fmaxf(mx, other_half(mx));
+        const float mn = fmaxf(m, mx);
+        const float f = __builtin_amdgcn_exp2f((m - mn) * c);
+        m = mn;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] *= f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[b][e] = __builtin_amdgcn_exp2f((s[b][e] - m) * c);
+                l += s[b][e];
+            }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const bf16x8 p = pack_frag(s[b], x);
+#pragma unroll
+                for (int t = 0; t < HD / 32; ++t)
+                    o[t] = mfma(col_frag<HD>(sv, 32 * b + 16 * x, t, lane), p, o[t]);
+            }
+    }
+    l += other_half(l);
+    if (q0 + (lane & 31) >= sq.len) return;
+    const int64_t row = sq.begin + qi;
+    const float inv = 1.f / l;
+    uint16_t* out = O + row * ldo + h * a.hd;
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int ch = 32 * t + crow(e, lane);
+            if (ch < a.hd)
+                *reinterpret_cast<u32x2*>(out + ch) = u32x2{pack2(o[t][e] * inv, o[t][e + 1] * inv),
+                                                            pack2(o[t][e + 2] * inv, o[t][e + 3] * inv)};
+        }
+    if (lse && lane < 32) lse[(int64_t)h * a.T + row] = m * a.scale + kLn2 * __builtin_amdgcn_logf(l);
+}
+
+// dQ (and delta) of 128 queries: loops over the key tiles they see.
+template <int HD>
+__global__ __launch_bounds__(NT) void attn_dq_kernel(AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo,
+                                                     const float* __restrict__ lse, const uint16_t* __restrict__ dO,
+                                                     int64_t lddo, float* __restrict__ delta,
+                                                     uint16_t* __restrict__ dQ, int64_t lddq) {
+    constexpr int BN = 32;
+    __shared__ __attribute__((aligned(16))) uint16_t sk[BN * HD], sv[BN * HD];
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+    if (!sq.any) return;
+    const int h = blockIdx.y, kv = h / (a.n_heads / a.n_kv);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int q0 = sq.tile * BM + wave * 32;
+    const int qi = min(q0 + (lane & 31), sq.len - 1);
+    const int64_t row = sq.begin + qi;
+    const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
+    const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
+    bf16x8 qf[HD / 16], df[HD / 16];
+    hold<HD>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
+    hold<HD>(dO + row * lddo + h * a.hd, a.hd, lane, df);
+    float dl = 0.f;
+    {
+        bf16x8 of[HD / 16];
+        hold<HD>(O + row * ldo + h * a.hd, a.hd, lane, of);
+#pragma unroll
+        for (int s = 0; s < HD / 16; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dl += (float)of[s][e] * (float)df[s][e];
+        dl += other_half(dl);
+    }
+    const bool live = q0 + (lane & 31) < sq.len;
+    if (live && lane < 32) delta[(int64_t)h * a.T + row] = dl;
+    const float c = a.scale * kLog2e, L = lse[(int64_t)h * a.T + row] * kLog2e;
+    f32x16 g[HD / 32];
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t) g[t] = zero16();
+    const int keys = min((sq.tile + 1) * BM, sq.len);
+    for (int k0 = 0; k0 < keys; k0 += BN) {
+        __syncthreads();
+        stage<HD, BN, NT>(K, a.ldk, a.hd, k0, sq.len, sk);
+        stage<HD, BN, NT>(V, a.ldv, a.hd, k0, sq.len, sv);
+        __syncthreads();
+        if (k0 > q0 + 31) continue;
+        f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+        for (int u = 0; u < HD / 16; ++u) {
+            s = mfma(row_frag<HD>(sk, 0, u, lane), qf[u], s);
+            dp = mfma(row_frag<HD>(sv, 0, u, lane), df[u], dp);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float p = __builtin_amdgcn_exp2f(s[e] * c - L);
+            s[e] = k0 + crow(e, lane) > qi ? 0.f : p * (dp[e] - dl);
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const bf16x8 d = pack_frag(s, x);
+#pragma unroll
+            for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 16 * x, t, lane), d, g[t]);
+        }
+    }
+    if (!live) return;
+    uint16_t* out = dQ + row * lddq + h * a.hd;
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const int ch = 32 * t + crow(e, lane);
+            if (ch < a.hd)
+                *reinterpret_cast<u32x2*>(out + ch) =
+                    u32x2{pack2(g[t][e] * a.scale, g[t][e + 1] * a.scale),
+                          pack2(g[t][e + 2] * a.scale, g[t][e + 3] * a.scale)};
+        }
+}
+
+// dK and dV of 128 keys: loops over the query heads of their key/value head and the queries that see them,
+// in that order, so the sums have one order.
+template <int HD>
+__global__ __launch_bounds__(NT) void attn_dkv_kernel(AttnArgs a, const float* __restrict__ lse,
+                                                      const uint16_t* __restrict__ dO, int64_t lddo,
+                                                      const float* __restrict__ delta, uint16_t* __restrict__ dK,
+                                                      int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv) {
+    constexpr int BQ = 32;
+    __shared__ __attribute__((aligned(16))) uint16_t sqr[BQ * HD], sdo[BQ * HD];
+    __shared__ __attribute__((aligned(16))) float sl[BQ], sd[BQ];
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+    if (!sq.any) return;
+    const int kv = blockIdx.y, group = a.n_heads / a.n_kv;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int k0 = sq.tile * BM + wave * 32;
+    const int ki = min(k0 + (lane & 31), sq.len - 1);
+    bf16x8 kf[HD / 16], vf[HD / 16];
+    hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
+    hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
+    const float c = a.scale * kLog2e;
+    f32x16 gk[HD / 32], gv[HD / 32];
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t) gk[t] = gv[t] = zero16();
+    for (int h = kv * group; h < (kv + 1) * group; ++h) {
+        const uint16_t* Q = a.q + sq.begin * a.ldq + h * a.hd;
+        const uint16_t* D = dO + sq.begin * lddo + h * a.hd;
+        const float* Lr = lse + (int64_t)h * a.T + sq.begin;
+        const float* Dr = delta + (int64_t)h * a.T + sq.begin;
+        for (int q0 = sq.tile * BM; q0 < sq.len; q0 += BQ) {
+            __syncthreads();
+            stage<HD, BQ, NT>(Q, a.ldq, a.hd, q0, sq.len, sqr);
+            stage<HD, BQ, NT>(D, lddo, a.hd, q0, sq.len, sdo);
+            if (threadIdx.x < BQ) {
+                const int r = min(q0 + (int)threadIdx.x, sq.len - 1);
+                sl[threadIdx.x] = Lr[r] * kLog2e;
+                sd[threadIdx.x] = Dr[r];
+            }
+            __syncthreads();
+            if (q0 + BQ - 1 < k0) continue;
+            f32x16 s = zero16(), dp = zero16();
+#pragma unroll
+            for (int u = 0; u < HD / 16; ++u) {
+                s = mfma(row_frag<HD>(sqr, 0, u, lane), kf[u], s);
+                dp = mfma(row_frag<HD>(sdo, 0, u, lane), vf[u], dp);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = crow(e, lane), qi = q0 + r;
+                const float p = qi < ki || qi >= sq.len ? 0.f : __builtin_amdgcn_exp2f(s[e] * c - sl[r]);
+                s[e] = p;
+                dp[e] = p * (dp[e] - sd[r]);
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const bf16x8 p = pack_frag(s, x), d = pack_frag(dp, x);
+#pragma unroll
+                for (int t = 0; t < HD / 32; ++t) {
+                    gv[t] = mfma(p, col_frag<HD>(sdo, 16 * x, t, lane), gv[t]);
+                    gk[t] = mfma(d, col_frag<HD>(sqr, 16 * x, t, lane), gk[t]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int r = k0 + crow(e, lane), ch = 32 * t + (lane & 31);
+            if (r >= sq.len || ch >= a.hd) continue;
+            const int64_t at = sq.begin + r;
+            dK[at * lddk + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)(gk[t][e] * a.scale));
+            dV[at * lddv + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)gv[t][e]);
+        }
+}
+
+#define RQ_HEAD_DIM(KERNEL, GRID, ...)                                                              \
+    do {                                                                                            \
+        if (a.hd <= 64) hipLaunchKernelGGL(KERNEL<64>, GRID, dim3(NT), 0, st, __VA_ARGS__);         \
+        else if (a.hd <= 128) hipLaunchKernelGGL(KERNEL<128>, GRID, dim3(NT), 0, st, __VA_ARGS__);  \
+        else hipLaunchKernelGGL(KERNEL<256>, GRID, dim3(NT), 0, st, __VA_ARGS__);                   \
+    } while (0)
+
+hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st) {
+    const dim3 grid((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_heads);
+    RQ_HEAD_DIM(attn_forward_kernel, grid, a, O, ldo, lse);
+    return hipGetLastError();
+}
+
+hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ldo, const float* lse,
+                                const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ, int64_t lddq,
+                                uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st) {
+    const dim3 gq((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_heads);
+    const dim3 gk((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_kv);
+    RQ_HEAD_DIM(attn_dq_kernel, gq, a, O, ldo, lse, dO, lddo, delta, dQ, lddq);
+    if (const hipError_t e = hipGetLastError()) return e;
+    RQ_HEAD_DIM(attn_dkv_kernel, gk, a, lse, dO, lddo, delta, dK, lddk, dV, lddv);
+    return hipGetLastError();
+}
+
+}  // namespace realq

@@ -314,4 +314,50 @@ struct CholArgs {
 };
 hipError_t chol_inverse(const CholArgs& c, hipStream_t st);
 
+// ---------------------------------------------------------------- token log probabilities
+struct LogprobsArgs {
+    const void* logits;  // [T][ld], V columns
+    bool f32;            // float32, else bf16
+    int64_t T, V, ld;
+    const int64_t* targets;  // [T] or NULL
+    int top;
+};
+size_t logprobs_workspace(int64_t T, int64_t V, int top, bool f32, int cus);
+hipError_t logprobs_forward(const LogprobsArgs& a, float* logp, float* lse, float* entropy, int64_t* top_ids,
+                            float* top_logp, void* work, int cus, hipStream_t st);
+hipError_t logprobs_backward(const LogprobsArgs& a, const float* lse, const float* entropy, const int64_t* top_ids,
+                             const float* dlogp, const float* dentropy, const float* dtop, void* dlogits, int64_t ldd,
+                             hipStream_t st);
+
+// ---------------------------------------------------------------- 8-bit integer product
+hipError_t quantize_rows_i8(const void* X, bool f32, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq,
+                            float* s, hipStream_t st);
+struct LinearI8Args {
+    const int8_t* X;  // [T][ldx]
+    const int8_t* W;  // [m][ldw]
+    int64_t T, n, m, ldx, ldw, ldy;
+    const float* sx;    // [T]
+    const float* sw;    // [m]
+    const float* bias;  // [m] or NULL
+    void* Y;            // [T][ldy]
+    bool f32;           // float32, else bf16
+};
+hipError_t linear_i8(const LinearI8Args& a, hipStream_t st);
+
+// ---------------------------------------------------------------- packed attention
+struct AttnArgs {
+    const uint16_t* q;  // [T][ldq], n_heads heads of hd channels
+    const uint16_t* k;
+    const uint16_t* v;
+    int64_t ldq, ldk, ldv, T, n_seqs;
+    const int32_t* cu;  // [n_seqs + 1]
+    int n_heads, n_kv, hd;
+    float scale;
+};
+hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st);
+// delta: [n_heads][T] workspace
+hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ldo, const float* lse,
+                                const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ, int64_t lddq,
+                                uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st);
+
 }  // namespace realq

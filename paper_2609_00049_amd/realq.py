@@ -38,6 +38,9 @@ EXPORTS = [
     "realq_bgd_step", "realq_bgd_loss", "realq_quantize_layer",
     "realq_pullback_metric", "realq_handoff", "realq_mlp_block_sweep",
     "realq_decoder_block_sweep", "realq_decoder_forward", "realq_mfma_peak",
+    "realq_token_logprobs_workspace", "realq_token_logprobs", "realq_token_logprobs_backward",
+    "realq_packed_attention", "realq_packed_attention_backward",
+    "realq_quantize_rows_i8", "realq_linear_i8",
 ]
 
 
@@ -126,6 +129,18 @@ class DecoderFwdOut(ctypes.Structure):
                 ("O", ctypes.c_void_p), ("x2", ctypes.c_void_p), ("y", ctypes.c_void_p)]
 
 
+class LogprobsDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("V", ctypes.c_int64), ("ld", ctypes.c_int64), ("logits", ctypes.c_void_p),
+                ("targets", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("top", ctypes.c_int32)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("n_seqs", ctypes.c_int64), ("n_heads", ctypes.c_int32),
+                ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("cu_seqlens", ctypes.c_void_p), ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("ldk", ctypes.c_int64), ("ldv", ctypes.c_int64)]
+
+
 def _load():
     if not _LIB_PATH.exists():
         raise ImportError(f"{_LIB_PATH} is not built; run paper_2609_00049_amd.build.build() first")
@@ -164,6 +179,17 @@ def _load():
         "realq_decoder_block_sweep": (ctypes.c_int, [vp, ctypes.POINTER(DecoderDesc), ctypes.POINTER(DecoderOut)]),
         "realq_decoder_forward": (ctypes.c_int, [vp, ctypes.POINTER(DecoderDesc), ctypes.POINTER(DecoderFwdOut)]),
         "realq_mfma_peak": (ctypes.c_int, [vp, i64, ctypes.POINTER(ctypes.c_double)]),
+        "realq_token_logprobs_workspace": (ctypes.c_int, [vp, ctypes.POINTER(LogprobsDesc),
+                                                          ctypes.POINTER(ctypes.c_size_t)]),
+        "realq_token_logprobs": (ctypes.c_int, [vp, ctypes.POINTER(LogprobsDesc), vp, vp, vp, vp, vp, vp,
+                                                ctypes.c_size_t]),
+        "realq_token_logprobs_backward": (ctypes.c_int, [vp, ctypes.POINTER(LogprobsDesc), vp, vp, vp, vp, vp, vp, vp,
+                                                         i64]),
+        "realq_packed_attention": (ctypes.c_int, [vp, ctypes.POINTER(AttentionDesc), vp, i64, vp]),
+        "realq_packed_attention_backward": (ctypes.c_int, [vp, ctypes.POINTER(AttentionDesc), vp, i64, vp, vp, i64, vp,
+                                                           vp, i64, vp, i64, vp, i64]),
+        "realq_quantize_rows_i8": (ctypes.c_int, [vp, vp, i32, i64, i64, i64, vp, i64, vp]),
+        "realq_linear_i8": (ctypes.c_int, [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -625,3 +651,200 @@ def decoder_forward(ctx: Context, X, blk: dict, *, n_heads, n_kv, head_dim, seq_
     o = DecoderFwdOut(*[_ptr(res.get(k)) for k in ("h1", "q", "k", "v", "O", "x2", "y")])
     ctx.check(_lib.realq_decoder_forward(ctx.h, ctypes.byref(desc), ctypes.byref(o)))
     return res
+
+
+# ----------------------------------------------------------------------------- running, scoring, differentiating
+#
+# Work goes on the context's stream, scratch memory and outputs that are not given come from torch's
+# allocator on that stream.  Rows may be strided (a slice of a wider tensor); the last axis is contiguous.
+
+I8, I64, I32 = torch.int8, torch.int64, torch.int32
+LOGPROBS_MAX_TOP = 64
+_DTYPE = {torch.bfloat16: 0, torch.float32: 1}
+
+
+def _check(t, name: str, dtypes, shape):
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch.Tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _use(ctx: Context, t: torch.Tensor, name: str):
+    """Device address of a tensor that a call on the context's stream reads or writes."""
+    if t.device != ctx.stream.device:
+        raise ValueError(f"{name} must be on {ctx.stream.device}, got {t.device}")
+    if torch.cuda.current_stream(t.device).cuda_stream != ctx.stream.cuda_stream:
+        t.record_stream(ctx.stream)  # its memory is not given out again before this stream is through
+    return t.data_ptr()
+
+
+def _flat(ctx: Context, t, name: str, dtypes, shape):
+    """A contiguous tensor, or None."""
+    if t is None:
+        return None
+    _check(t, name, dtypes, shape)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return _use(ctx, t, name)
+
+
+def _rows(ctx: Context, t, name: str, dtypes, shape):
+    """(address, elements between rows) of a tensor whose rows (the axes after the first) are contiguous."""
+    _check(t, name, dtypes, shape)
+    width = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != width:
+            raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
+        width *= size
+    ld = t.stride(0) if t.shape[0] > 1 else -(-width // 16) * 16
+    if ld < width:
+        raise ValueError(f"the rows of {name} overlap: strides {t.stride()}")
+    return _use(ctx, t, name), ld
+
+
+def _new(ctx: Context, shape, dtype) -> torch.Tensor:
+    if torch.cuda.current_stream(ctx.stream.device).cuda_stream == ctx.stream.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=ctx.stream.device)
+    with torch.cuda.stream(ctx.stream):
+        return torch.empty(shape, dtype=dtype, device=ctx.stream.device)
+
+
+@dataclass
+class TokenLogprobs:
+    logp: Optional[torch.Tensor]       # [T] float32, None without targets
+    lse: torch.Tensor                  # [T] float32
+    entropy: Optional[torch.Tensor]    # [T] float32
+    top_ids: Optional[torch.Tensor]    # [T, top] int64
+    top_logp: Optional[torch.Tensor]   # [T, top] float32
+
+
+def token_logprobs(ctx: Context, logits, targets=None, *, top: int = 0, entropy: bool = False) -> TokenLogprobs:
+    """Log probabilities of ``targets`` [T] (int64; below 0: no token) under ``logits`` [T, V] (bf16 or
+    float32), each row's log-sum-exp, on request its entropy and its ``top`` likeliest tokens (ties by the
+    lower one)."""
+    T, V = _dims(logits, "logits", 2)
+    _check(logits, "logits", (BF16, F32), (T, V))
+    if not 0 <= top <= min(V, LOGPROBS_MAX_TOP):
+        raise ValueError(f"top must be 0 .. {min(V, LOGPROBS_MAX_TOP)}, got {top}")
+    y = _flat(ctx, targets, "targets", (I64,), (T,))
+    z, ld = _rows(ctx, logits, "logits", (BF16, F32), (T, V))
+    r = TokenLogprobs(logp=None if targets is None else _new(ctx, (T,), F32), lse=_new(ctx, (T,), F32),
+                      entropy=_new(ctx, (T,), F32) if entropy else None,
+                      top_ids=_new(ctx, (T, top), I64) if top else None,
+                      top_logp=_new(ctx, (T, top), F32) if top else None)
+    desc = LogprobsDesc(T, V, ld, z, y, _DTYPE[logits.dtype], top)
+    need = ctypes.c_size_t()
+    ctx.check(_lib.realq_token_logprobs_workspace(ctx.h, ctypes.byref(desc), ctypes.byref(need)))
+    work = _new(ctx, (need.value,), U8) if need.value else None
+    ctx.check(_lib.realq_token_logprobs(ctx.h, ctypes.byref(desc), *(t.data_ptr() if t is not None else None for t in (
+        r.logp, r.lse, r.entropy, r.top_ids, r.top_logp, work)), need.value))
+    return r
+
+
+def token_logprobs_backward(ctx: Context, logits, targets, scores: TokenLogprobs, *, dlogp=None, dentropy=None,
+                            dtop=None, out=None) -> torch.Tensor:
+    """Gradient at the logits of a loss with derivatives ``dlogp`` [T], ``dentropy`` [T] and ``dtop`` [T, top]
+    (each may be None) with respect to ``scores``, what token_logprobs gave for these logits and targets.
+    ``out`` [T, V] (the logits' type; the logits themselves are allowed) receives it."""
+    T, V = _dims(logits, "logits", 2)
+    _check(logits, "logits", (BF16, F32), (T, V))
+    if dentropy is not None and scores.entropy is None:
+        raise ValueError("dentropy needs scores with entropy=True")
+    if dtop is not None and scores.top_ids is None:
+        raise ValueError("dtop needs scores with top >= 1")
+    if dlogp is not None and targets is None:
+        raise ValueError("dlogp needs targets")
+    top = 0 if scores.top_ids is None else _dims(scores.top_ids, "scores.top_ids", 2)[1]
+    y = _flat(ctx, targets, "targets", (I64,), (T,))
+    args = (_flat(ctx, scores.lse, "scores.lse", (F32,), (T,)), _flat(ctx, scores.entropy, "scores.entropy", (F32,), (T,)),
+            _flat(ctx, scores.top_ids, "scores.top_ids", (I64,), (T, top)), _flat(ctx, dlogp, "dlogp", (F32,), (T,)),
+            _flat(ctx, dentropy, "dentropy", (F32,), (T,)), _flat(ctx, dtop, "dtop", (F32,), (T, top)))
+    z, ld = _rows(ctx, logits, "logits", (BF16, F32), (T, V))
+    if out is None:
+        out = _new(ctx, (T, V), logits.dtype)
+    d, ldd = _rows(ctx, out, "out", (logits.dtype,), (T, V))
+    desc = LogprobsDesc(T, V, ld, z, y, _DTYPE[logits.dtype], top)
+    ctx.check(_lib.realq_token_logprobs_backward(ctx.h, ctypes.byref(desc), *args, d, ldd))
+    return out
+
+
+def _attention_desc(ctx: Context, q, k, v, cu_seqlens, scale):
+    T, H, hd = _dims(q, "q", 3)
+    G = _dims(k, "k", 3)[1]
+    (B,) = _dims(cu_seqlens, "cu_seqlens", 1)
+    if B < 1:
+        raise ValueError("cu_seqlens must hold at least one offset")
+    pq, ldq = _rows(ctx, q, "q", (BF16,), (T, H, hd))
+    pk, ldk = _rows(ctx, k, "k", (BF16,), (T, G, hd))
+    pv, ldv = _rows(ctx, v, "v", (BF16,), (T, G, hd))
+    return AttentionDesc(T, B - 1, H, G, hd, 0.0 if scale is None else scale,
+                         _flat(ctx, cu_seqlens, "cu_seqlens", (I32,), (B,)), pq, pk, pv, ldq, ldk, ldv)
+
+
+def packed_attention(ctx: Context, q, k, v, cu_seqlens, *, scale: Optional[float] = None, out=None):
+    """Causal attention of packed sequences: q [T, n_heads, head_dim], k and v [T, n_kv, head_dim] bf16 (heads of
+    a token in one row, rows may be strided), cu_seqlens [n_seqs + 1] int32 on the device.  Returns (out, lse):
+    out like q (rows outside every sequence are left as they were), lse [n_heads, T] float32.  scale:
+    1 / sqrt(head_dim) by default."""
+    desc = _attention_desc(ctx, q, k, v, cu_seqlens, scale)
+    if out is None:
+        out = _new(ctx, q.shape, BF16)
+    o, ldo = _rows(ctx, out, "out", (BF16,), q.shape)
+    lse = _new(ctx, (desc.n_heads, desc.T), F32)
+    ctx.check(_lib.realq_packed_attention(ctx.h, ctypes.byref(desc), o, ldo, lse.data_ptr()))
+    return out, lse
+
+
+def packed_attention_backward(ctx: Context, q, k, v, cu_seqlens, out, lse, dout, *, scale: Optional[float] = None,
+                              dq=None, dk=None, dv=None):
+    """(dq, dk, dv), bf16 like q, k and v, from what packed_attention gave and dout, the gradient at out; dk and
+    dv are summed over the query heads that share them.  dq, dk, dv may be given (rows may be strided)."""
+    desc = _attention_desc(ctx, q, k, v, cu_seqlens, scale)
+    o, ldo = _rows(ctx, out, "out", (BF16,), q.shape)
+    d, lddo = _rows(ctx, dout, "dout", (BF16,), q.shape)
+    pl = _flat(ctx, lse, "lse", (F32,), (desc.n_heads, desc.T))
+    dq = _new(ctx, q.shape, BF16) if dq is None else dq
+    dk = _new(ctx, k.shape, BF16) if dk is None else dk
+    dv = _new(ctx, v.shape, BF16) if dv is None else dv
+    delta = _new(ctx, (desc.n_heads, desc.T), F32)
+    ctx.check(_lib.realq_packed_attention_backward(
+        ctx.h, ctypes.byref(desc), o, ldo, pl, d, lddo, delta.data_ptr(), *_rows(ctx, dq, "dq", (BF16,), q.shape),
+        *_rows(ctx, dk, "dk", (BF16,), k.shape), *_rows(ctx, dv, "dv", (BF16,), v.shape)))
+    return dq, dk, dv
+
+
+def quantize_rows_i8(ctx: Context, X, out=None):
+    """(codes [T, n] int8, scales [T] float32) of the rows of X [T, n] (bf16 or float32): scale max|x| / 127, codes
+    to nearest even.  Codes that are not given ``out`` are laid out with rows on 16 bytes."""
+    T, n = _dims(X, "X", 2)
+    x, ldx = _rows(ctx, X, "X", (BF16, F32), (T, n))
+    if out is None:
+        out = _new(ctx, (T, -(-n // 16) * 16), I8)
+        if n % 16:
+            out = out[:, :n]
+    q, ldq = _rows(ctx, out, "out", (I8,), (T, n))
+    s = _new(ctx, (T,), F32)
+    ctx.check(_lib.realq_quantize_rows_i8(ctx.h, x, _DTYPE[X.dtype], T, n, ldx, q, ldq, s.data_ptr()))
+    return out, s
+
+
+def linear_i8(ctx: Context, Xq, sx, Wq, sw, *, bias=None, dtype=torch.bfloat16, out=None) -> torch.Tensor:
+    """[T, m] = sx_t sw_i sum_j Xq[t, j] Wq[i, j] (+ bias_i), exact integer sums, in ``dtype`` (bf16 or float32) or
+    into ``out``.  Xq [T, n], Wq [m, n] int8 (a module quantized per row: codes - zeros); sx [T], sw [m], bias [m]
+    float32."""
+    T, n = _dims(Xq, "Xq", 2)
+    m = _dims(Wq, "Wq", 2)[0]
+    x, ldx = _rows(ctx, Xq, "Xq", (I8,), (T, n))
+    w, ldw = _rows(ctx, Wq, "Wq", (I8,), (m, n))
+    if out is None:
+        if dtype not in _DTYPE:
+            raise ValueError(f"dtype must be torch.bfloat16 or torch.float32, got {dtype}")
+        out = _new(ctx, (T, m), dtype)
+    y, ldy = _rows(ctx, out, "out", (BF16, F32), (T, m))
+    ctx.check(_lib.realq_linear_i8(ctx.h, x, ldx, _flat(ctx, sx, "sx", (F32,), (T,)), w, ldw,
+                                   _flat(ctx, sw, "sw", (F32,), (m,)), _flat(ctx, bias, "bias", (F32,), (m,)), T, n, m,
+                                   y, _DTYPE[out.dtype], ldy))
+    return out
