@@ -4,6 +4,8 @@
 //   Y[t, i] = s_t c_i sum_j q_tj w_ij (+ b_i)
 //
 // The sums are exact in 32-bit integers (j < 2^17 columns of magnitude at most 2^14 each).
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -35,27 +37,29 @@ constexpr int QT = 256;
 }  // namespace
 
 template <class E>
-__global__ __launch_bounds__(QT) void quantize_rows_kernel(const E* __restrict__ X, int64_t n, int64_t ldx,
+__global__ __launch_bounds__(QT) void quantize_rows_kernel(const E* __restrict__ X, int64_t T, int64_t n, int64_t ldx,
                                                            int8_t* __restrict__ Q, int64_t ldq,
                                                            float* __restrict__ S) {
     __shared__ uint32_t red[QT / 64];
-    const int64_t t = blockIdx.x;
-    const E* x = X + t * ldx;
-    auto at = [&](int64_t j) {
-        if constexpr (sizeof(E) == 2) return bf2f(x[j]);
-        else return x[j];
-    };
-    // the bits of |x| keep its order, infinities and NaN above all finite values
-    uint32_t m = 0;
-    for (int64_t j = threadIdx.x; j < n; j += QT) m = max(m, __float_as_uint(at(j)) & 0x7FFFFFFFu);
-    for (int w = 32; w > 0; w >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    for (int w = 0; w < QT / 64; ++w) m = max(m, red[w]);
-    const bool finite = m < 0x7F800000u;
-    const float s = finite ? __uint_as_float(m) / 127.f : NAN;
-    if (threadIdx.x == 0) S[t] = s;
-    for (int64_t j = threadIdx.x; j < n; j += QT) Q[t * ldq + j] = (int8_t)(s > 0.f ? (int)code_of(at(j), s) : 0);
+    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+        const E* x = X + t * ldx;
+        auto at = [&](int64_t j) {
+            if constexpr (sizeof(E) == 2) return bf2f(x[j]);
+            else return x[j];
+        };
+        // the bits of |x| keep its order, infinities and NaN above all finite values
+        uint32_t m = 0;
+        for (int64_t j = threadIdx.x; j < n; j += QT) m = max(m, __float_as_uint(at(j)) & 0x7FFFFFFFu);
+        for (int w = 32; w > 0; w >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w));
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+        for (int w = 0; w < QT / 64; ++w) m = max(m, red[w]);
+        const bool finite = m < 0x7F800000u;
+        const float s = finite ? __uint_as_float(m) / 127.f : NAN;
+        if (threadIdx.x == 0) S[t] = s;
+        for (int64_t j = threadIdx.x; j < n; j += QT) Q[t * ldq + j] = (int8_t)(s > 0.f ? (int)code_of(at(j), s) : 0);
+        __syncthreads();
+    }
 }
 
 // 128 x 128 tile (weights x tokens), 4 waves of 64 x 64, v_mfma_i32_32x32x32_i8; any strides and alignment.
@@ -131,11 +135,12 @@ __global__ __launch_bounds__(256) void linear_i8_kernel(const int8_t* __restrict
 
 hipError_t quantize_rows_i8(const void* X, bool f32, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq,
                             float* s, hipStream_t st) {
+    const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
     if (f32)
-        hipLaunchKernelGGL(quantize_rows_kernel<float>, dim3((unsigned)T), dim3(QT), 0, st, (const float*)X, n, ldx, Q,
+        hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, dim3(QT), 0, st, (const float*)X, T, n, ldx, Q,
                            ldq, s);
     else
-        hipLaunchKernelGGL(quantize_rows_kernel<uint16_t>, dim3((unsigned)T), dim3(QT), 0, st, (const uint16_t*)X, n,
+        hipLaunchKernelGGL(quantize_rows_kernel<uint16_t>, grid, dim3(QT), 0, st, (const uint16_t*)X, T, n,
                            ldx, Q, ldq, s);
     return hipGetLastError();
 }
