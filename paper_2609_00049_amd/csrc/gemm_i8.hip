@@ -14,6 +14,9 @@ namespace realq {
 namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
 // The whole number nearest x / s, ties to even, for |x| <= 127.5 s or so: the float32 quotient's rounding can
@@ -30,6 +33,27 @@ __device__ __forceinline__ float code_of(float x, float s) {
     if (r > h || (r == h && odd)) q += 1.f;
     else if (r < -h || (r == -h && odd)) q -= 1.f;
     return fminf(fmaxf(q, -127.f), 127.f);
+}
+
+// y[0..count) to p, `wide`: p is aligned to 4 elements
+__device__ __forceinline__ void put4(uint16_t* p, const float (&y)[4], bool wide, int count) {
+    const f32x2 a = {y[0], y[1]}, b = {y[2], y[3]};
+    const u32x2 v = {__builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2)),
+                     __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2))};
+    if (wide && count >= 4) {
+        *reinterpret_cast<u32x2*>(p) = v;
+    } else {
+        for (int x = 0; x < 4; ++x)
+            if (x < count) p[x] = (uint16_t)(v[x >> 1] >> (16 * (x & 1)));
+    }
+}
+__device__ __forceinline__ void put4(float* p, const float (&y)[4], bool wide, int count) {
+    if (wide && count >= 4) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{y[0], y[1], y[2], y[3]};
+    } else {
+        for (int x = 0; x < 4; ++x)
+            if (x < count) p[x] = y[x];
+    }
 }
 
 constexpr int QT = 256;
@@ -133,6 +157,246 @@ __global__ __launch_bounds__(256) void linear_i8_kernel(const int8_t* __restrict
     }
 }
 
+// ---------------------------------------------------------------- prompts: operands on 16 bytes
+// BM weight rows x BN tokens a block, 64 x 128 a wave.  K advances in slices of 64 columns through a ring
+// of three LDS stages filled by direct-to-LDS 16-byte loads: slice s + 2 is in flight while slice s is
+// multiplied.  16-byte chunk c of LDS row r lies at c ^ f(r), so the rows a fragment read touches fall on
+// distinct banks.
+namespace {
+
+constexpr int SL = 64;  // columns (bytes) of a slice
+
+__device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ ((r >> 1) ^ (r >> 3))) & 3; }
+// lane i fills LDS bytes lds + 16 i .. + 15 from base + its own byte offset; completion is waited for by the
+// vmcnt counts of the K loop, not by the compiler
+__device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)p; }
+
+// Tile of block b: each XCD (blocks are dealt to the 8 round-robin) owns one run of tiles, walked in bands of
+// `band` weight tiles so that a band's weights and a few token tiles stay in its L2.
+__device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64_t band, int64_t& i, int64_t& j) {
+    const int64_t n = tm * tn, q = n >> 3, r = n & 7, x = b & 7;
+    const int64_t L = x * q + min(x, r) + (b >> 3);
+    const int64_t g = L / (band * tn), first = g * band, rows = min(band, tm - first), in = L - g * band * tn;
+    i = first + in % rows;
+    j = in / rows;
+}
+
+}  // namespace
+
+template <int WM, int WN, class E>
+__global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
+    const int8_t* __restrict__ W, int64_t ldw, const int8_t* __restrict__ X, int64_t ldx, int64_t m, int64_t T,
+    int64_t n, const float* __restrict__ sx, const float* __restrict__ sw, const float* __restrict__ bias,
+    E* __restrict__ Y, int64_t ldy, int64_t tm, int64_t tn, int64_t band) {
+    constexpr int BM = 64 * WM, BN = 128 * WN, NW = WM * WN, NT = 64 * NW;
+    constexpr int RA = BM / 16 / NW, RB = BN / 16 / NW;  // 1 KB runs (16 rows) a wave loads of each operand
+    __shared__ __attribute__((aligned(16))) int8_t st0[(BM + BN) * SL], st1[(BM + BN) * SL], st2[(BM + BN) * SL];
+    __shared__ __attribute__((aligned(16))) float rows[2 * BM];  // the tile's output scales and biases
+    int64_t ti, tj;
+    tile_of(blockIdx.x, tm, tn, band, ti, tj);
+    const int64_t i0 = ti * BM, t0 = tj * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN * 64, wn = wave % WN * 128;
+    i32x16 acc[2][4];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
+    // each lane's source offsets; rows past the end read the last one, into results that are not stored
+    uint32_t oa[RA], ob[RB];
+    const int lr = lane >> 2;
+#pragma unroll
+    for (int q = 0; q < RA; ++q) {
+        const int r = 16 * (wave + NW * q) + lr;
+        oa[q] = (uint32_t)((min(i0 + r, m - 1) - i0) * ldw + 16 * chunk_at(r, lane));
+    }
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+        const int r = 16 * (wave + NW * q) + lr;
+        ob[q] = (uint32_t)((min(t0 + r, T - 1) - t0) * ldx + 16 * chunk_at(r, lane));
+    }
+    const int8_t* const bw = W + i0 * ldw;
+    const int8_t* const bx = X + t0 * ldx;
+    const uint32_t at[3] = {lds_at(st0), lds_at(st1), lds_at(st2)};
+    auto issue = [&](int64_t s, uint32_t stage) {
+#pragma unroll
+        for (int q = 0; q < RA; ++q) to_lds(bw + s * SL, oa[q], stage + (wave + NW * q) * 1024);
+#pragma unroll
+        for (int q = 0; q < RB; ++q) to_lds(bx + s * SL, ob[q], stage + BM * SL + (wave + NW * q) * 1024);
+    };
+    auto frag = [&](const int8_t* st, int row, int c) {
+        return *reinterpret_cast<const i32x4*>(st + row * SL + 16 * chunk_at(row, c));
+    };
+    auto multiply = [&](const int8_t* st) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            i32x4 a[2], b[4];
+            const int c = 2 * k + (lane >> 5);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) a[i] = frag(st, wm + 32 * i + (lane & 31), c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+        }
+    };
+    const int64_t full = n / SL;
+    for (int r = threadIdx.x; r < BM; r += NT) {
+        rows[r] = sw[min(i0 + r, m - 1)];
+        rows[BM + r] = bias ? bias[min(i0 + r, m - 1)] : 0.f;
+    }
+    if (n % SL) {  // the last columns first, zeros behind them
+        const int64_t k0 = full * SL;
+        for (int c = threadIdx.x; c < (BM + BN) * 4; c += NT) {
+            const int r = c >> 2;
+            const bool w = r < BM;
+            const int64_t k = k0 + 16 * (c & 3);
+            const int8_t* p = w ? W + min(i0 + r, m - 1) * ldw + k : X + min(t0 + r - BM, T - 1) * ldx + k;
+            i32x4 v = {0, 0, 0, 0};
+            if (k + 16 <= n) {
+                v = *reinterpret_cast<const i32x4*>(p);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[e] << (8 * (e & 3)));
+            }
+            const int rr = w ? r : r - BM;
+            *reinterpret_cast<i32x4*>(st0 + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
+        }
+        __syncthreads();
+        multiply(st0);
+        __syncthreads();
+    }
+    if constexpr (NW == 8) {
+        // Two waves share a SIMD, one of each group of 4.  Between two barriers one group multiplies a slice
+        // from registers while the other reads its next fragments and issues loads, so the matrix unit has
+        // work while a wave waits for LDS: group 1 enters the loop one barrier later.  Slice s lies in stage
+        // s % 3; a wave loads its part of slice s + 2 into the stage of slice s - 1, which both groups have
+        // read, and waits until its part of slice s + 1 has landed, before either group reads that.
+        const int group = wave >> 2;
+        auto fetch = [&](int64_t s, const int8_t* st, uint32_t refill, i32x4 (&a)[2][2], i32x4 (&b)[2][4]) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int c = 2 * k + (lane >> 5);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) a[k][i] = frag(st, wm + 32 * i + (lane & 31), c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) b[k][j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
+            }
+            if (s + 2 < full) issue(s + 2, refill);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (s + 2 < full) vm_wait<RA + RB>();
+            else vm_wait<0>();
+        };
+        auto slice = [&](int64_t s, const int8_t* st, uint32_t refill) {
+            i32x4 a[2][2], b[2][4];
+            fetch(s, st, refill, a, b);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[k][i], b[k][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if (full > 0) issue(0, at[0]);
+        if (full > 1) issue(1, at[1]);
+        if (full > 1) vm_wait<RA + RB>();
+        else vm_wait<0>();
+        __builtin_amdgcn_s_barrier();
+        if (group == 1) __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        for (int64_t s = 0; s < full; s += 3) {
+            slice(s, st0, at[2]);
+            if (s + 1 >= full) break;
+            slice(s + 1, st1, at[0]);
+            if (s + 2 >= full) break;
+            slice(s + 2, st2, at[1]);
+        }
+        if (group == 0) __builtin_amdgcn_s_barrier();
+    } else {
+        // slice s: its loads have landed, everyone's are visible and nobody reads the stage of slice s - 1 any more
+        auto step = [&](int64_t s, const int8_t* st, uint32_t refill) {
+            if (s + 1 < full) vm_wait<RA + RB>();
+            else vm_wait<0>();
+            __builtin_amdgcn_s_barrier();
+            if (s + 2 < full) issue(s + 2, refill);
+            multiply(st);
+        };
+        if (full > 0) issue(0, at[0]);
+        if (full > 1) issue(1, at[1]);
+        for (int64_t s = 0; s < full; s += 3) {
+            step(s, st0, at[2]);
+            if (s + 1 >= full) break;
+            step(s + 1, st1, at[0]);
+            if (s + 2 >= full) break;
+            step(s + 2, st2, at[1]);
+        }
+    }
+    // The wave's 64 outputs of 32 tokens at a time, through LDS of its own so that the stores are whole lines:
+    // a lane holds one token and 4 consecutive outputs, and stores 16 bytes of a token's 64 outputs.
+    constexpr int PER = 16 / (int)sizeof(E), LPR = 64 / PER, ROW = 64 + PER;  // lanes per token, elements per LDS row
+    static_assert((NW + 2) / 3 * 32 * ROW * (int)sizeof(E) <= (BM + BN) * SL, "the stages hold the outputs");
+    __syncthreads();
+    E* const own = reinterpret_cast<E*>(wave % 3 == 0 ? st0 : wave % 3 == 1 ? st1 : st2) + wave / 3 * (32 * ROW);
+    const bool wide = ldy % PER == 0 && ((uintptr_t)Y & 15) == 0;
+    const int64_t r0 = i0 + wm;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t tb = t0 + wn + 32 * j;
+        const float st = sx[min(tb + (lane & 31), T - 1)];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int c = 32 * i + 8 * (e >> 2) + 4 * (lane >> 5);
+                const f32x4 w = *reinterpret_cast<const f32x4*>(rows + wm + c);
+                float y[4];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) y[x] = (float)acc[i][j][e + x] * st * w[x];
+                if (bias) {
+                    const f32x4 b = *reinterpret_cast<const f32x4*>(rows + BM + wm + c);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) y[x] += b[x];
+                }
+                put4(own + (lane & 31) * ROW + c, y, true, 4);
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (wide && r0 + 64 <= m) {
+            const int c = lane % LPR * PER;
+#pragma unroll
+            for (int q = 0; q < LPR / 2; ++q) {
+                const int row = q * (64 / LPR) + lane / LPR;
+                const i32x4 v = *reinterpret_cast<const i32x4*>(own + row * ROW + c);
+                if (tb + row < T) *reinterpret_cast<i32x4*>(Y + (tb + row) * ldy + r0 + c) = v;
+            }
+        } else {  // an output a lane
+            const int rows_here = (int)min(T - tb, (int64_t)32);
+            if (r0 + lane < m)
+                for (int row = 0; row < rows_here; ++row) Y[(tb + row) * ldy + r0 + lane] = own[row * ROW + lane];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
 hipError_t quantize_rows_i8(const void* X, bool f32, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq,
                             float* s, hipStream_t st) {
     const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
@@ -145,16 +409,41 @@ hipError_t quantize_rows_i8(const void* X, bool f32, int64_t T, int64_t n, int64
     return hipGetLastError();
 }
 
-hipError_t linear_i8(const LinearI8Args& a, hipStream_t st) {
+namespace {
+
+template <class E>
+hipError_t simple(const LinearI8Args& a, hipStream_t st) {
     const int64_t tm = (a.m + SB - 1) / SB, tt = (a.T + SB - 1) / SB;
-    const dim3 grid((unsigned)(tm * tt));
-    if (a.f32)
-        hipLaunchKernelGGL(linear_i8_kernel<float>, grid, dim3(256), 0, st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx,
-                           a.sw, a.bias, (float*)a.Y, a.ldy, tm);
-    else
-        hipLaunchKernelGGL(linear_i8_kernel<uint16_t>, grid, dim3(256), 0, st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n,
-                           a.sx, a.sw, a.bias, (uint16_t*)a.Y, a.ldy, tm);
+    hipLaunchKernelGGL(linear_i8_kernel<E>, dim3((unsigned)(tm * tt)), dim3(256), 0, st, a.W, a.ldw, a.X, a.ldx, a.m,
+                       a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy, tm);
     return hipGetLastError();
+}
+
+template <int WM, int WN, class E>
+hipError_t tiled(const LinearI8Args& a, hipStream_t st) {
+    const int64_t tm = (a.m + 64 * WM - 1) / (64 * WM), tn = (a.T + 128 * WN - 1) / (128 * WN);
+    const char* be = getenv("RQ_BAND");
+    const int64_t band = be ? atoi(be) : 8;
+    hipLaunchKernelGGL((linear_i8_tile_kernel<WM, WN, E>), dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0, st, a.W,
+                       a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy, tm, tn, band);
+    return hipGetLastError();
+}
+
+template <class E>
+hipError_t linear(const LinearI8Args& a, hipStream_t st) {
+    const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && a.ldx % 16 == 0 && a.ldw % 16 == 0;
+    const char* v = getenv("RQ_TILE");
+    const int k = v ? atoi(v) : 1;
+    if (!on16 || a.T <= 64 || k == 0) return simple<E>(a, st);
+    if (k == 1) return tiled<2, 2, E>(a, st);
+    if (k == 2) return tiled<4, 2, E>(a, st);
+    return tiled<2, 1, E>(a, st);
+}
+
+}  // namespace
+
+hipError_t linear_i8(const LinearI8Args& a, hipStream_t st) {
+    return a.f32 ? linear<float>(a, st) : linear<uint16_t>(a, st);
 }
 
 }  // namespace realq

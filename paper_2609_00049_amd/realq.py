@@ -258,6 +258,7 @@ class Context:
     def __init__(self, stream: Optional[torch.cuda.Stream] = None):
         stream = stream or torch.cuda.current_stream()
         self.stream = stream
+        self.device, self.raw_stream = stream.device, stream.cuda_stream
         h = ctypes.c_void_p()
         rc = _lib.realq_ctx_create(ctypes.byref(h), ctypes.c_void_p(stream.cuda_stream))
         if rc != OK:
@@ -663,53 +664,68 @@ LOGPROBS_MAX_TOP = 64
 _DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 
 
-def _check(t, name: str, dtypes, shape):
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a torch.Tensor")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+# The raw handle of the stream that is current on a device, without making a Stream object.
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _use(ctx: Context, t: torch.Tensor, name: str):
-    """Device address of a tensor that a call on the context's stream reads or writes."""
-    if t.device != ctx.stream.device:
-        raise ValueError(f"{name} must be on {ctx.stream.device}, got {t.device}")
-    if torch.cuda.current_stream(t.device).cuda_stream != ctx.stream.cuda_stream:
-        t.record_stream(ctx.stream)  # its memory is not given out again before this stream is through
-    return t.data_ptr()
+class _Call:
+    """One call on a context: checks its tensors, gives their addresses and makes its outputs."""
+    __slots__ = ("ctx", "device", "foreign")
+
+    def __init__(self, ctx: Context):
+        self.ctx = ctx
+        self.device = ctx.device
+        # another stream is current: memory of the call must not be given out again, nor made, on that one
+        self.foreign = _current(ctx.device.index) != ctx.raw_stream
+
+    def use(self, t: torch.Tensor, name: str) -> int:
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, got {t.device}")
+        if self.foreign:
+            t.record_stream(self.ctx.stream)
+        return t.data_ptr()
+
+    @staticmethod
+    def check(t, name: str, dtypes, shape):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} must be a torch.Tensor")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+    def flat(self, t, name: str, dtypes, shape):
+        """Address of a contiguous tensor, or None."""
+        if t is None:
+            return None
+        self.check(t, name, dtypes, shape)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return self.use(t, name)
+
+    def rows(self, t, name: str, dtypes, shape):
+        """(address, elements between rows) of a tensor whose rows (the axes after the first) are contiguous."""
+        self.check(t, name, dtypes, shape)
+        if not t.is_contiguous():
+            width = 1
+            for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+                if size > 1 and stride != width:
+                    raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
+                width *= size
+            if t.shape[0] > 1:
+                if t.stride(0) < width:
+                    raise ValueError(f"the rows of {name} overlap: strides {t.stride()}")
+                return self.use(t, name), t.stride(0)
+        return self.use(t, name), math.prod(shape[1:])
+
+    def new(self, shape, dtype) -> torch.Tensor:
+        if not self.foreign:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.ctx.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
 
 
-def _flat(ctx: Context, t, name: str, dtypes, shape):
-    """A contiguous tensor, or None."""
-    if t is None:
-        return None
-    _check(t, name, dtypes, shape)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return _use(ctx, t, name)
-
-
-def _rows(ctx: Context, t, name: str, dtypes, shape):
-    """(address, elements between rows) of a tensor whose rows (the axes after the first) are contiguous."""
-    _check(t, name, dtypes, shape)
-    width = 1
-    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if size > 1 and stride != width:
-            raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
-        width *= size
-    ld = t.stride(0) if t.shape[0] > 1 else -(-width // 16) * 16
-    if ld < width:
-        raise ValueError(f"the rows of {name} overlap: strides {t.stride()}")
-    return _use(ctx, t, name), ld
-
-
-def _new(ctx: Context, shape, dtype) -> torch.Tensor:
-    if torch.cuda.current_stream(ctx.stream.device).cuda_stream == ctx.stream.cuda_stream:
-        return torch.empty(shape, dtype=dtype, device=ctx.stream.device)
-    with torch.cuda.stream(ctx.stream):
-        return torch.empty(shape, dtype=dtype, device=ctx.stream.device)
+_FLOAT, _BF, _F, _I8, _I64, _I32 = (BF16, F32), (BF16,), (F32,), (I8,), (I64,), (I32,)
 
 
 @dataclass
@@ -726,22 +742,22 @@ def token_logprobs(ctx: Context, logits, targets=None, *, top: int = 0, entropy:
     float32), each row's log-sum-exp, on request its entropy and its ``top`` likeliest tokens (ties by the
     lower one)."""
     T, V = _dims(logits, "logits", 2)
-    _check(logits, "logits", (BF16, F32), (T, V))
+    call = _Call(ctx)
+    z, ld = call.rows(logits, "logits", _FLOAT, (T, V))
     if not 0 <= top <= min(V, LOGPROBS_MAX_TOP):
         raise ValueError(f"top must be 0 .. {min(V, LOGPROBS_MAX_TOP)}, got {top}")
-    y = _flat(ctx, targets, "targets", (I64,), (T,))
-    z, ld = _rows(ctx, logits, "logits", (BF16, F32), (T, V))
-    r = TokenLogprobs(logp=None if targets is None else _new(ctx, (T,), F32), lse=_new(ctx, (T,), F32),
-                      entropy=_new(ctx, (T,), F32) if entropy else None,
-                      top_ids=_new(ctx, (T, top), I64) if top else None,
-                      top_logp=_new(ctx, (T, top), F32) if top else None)
+    y = call.flat(targets, "targets", _I64, (T,))
+    logp = None if targets is None else call.new((T,), F32)
+    lse = call.new((T,), F32)
+    ent = call.new((T,), F32) if entropy else None
+    ids, tops = (call.new((T, top), I64), call.new((T, top), F32)) if top else (None, None)
     desc = LogprobsDesc(T, V, ld, z, y, _DTYPE[logits.dtype], top)
-    need = ctypes.c_size_t()
-    ctx.check(_lib.realq_token_logprobs_workspace(ctx.h, ctypes.byref(desc), ctypes.byref(need)))
-    work = _new(ctx, (need.value,), U8) if need.value else None
-    ctx.check(_lib.realq_token_logprobs(ctx.h, ctypes.byref(desc), *(t.data_ptr() if t is not None else None for t in (
-        r.logp, r.lse, r.entropy, r.top_ids, r.top_logp, work)), need.value))
-    return r
+    ref, need = ctypes.byref(desc), ctypes.c_size_t()
+    ctx.check(_lib.realq_token_logprobs_workspace(ctx.h, ref, ctypes.byref(need)))
+    work = call.new((need.value,), U8) if need.value else None
+    ctx.check(_lib.realq_token_logprobs(ctx.h, ref, *[t if t is None else t.data_ptr() for t in (
+        logp, lse, ent, ids, tops, work)], need.value))
+    return TokenLogprobs(logp, lse, ent, ids, tops)
 
 
 def token_logprobs_backward(ctx: Context, logits, targets, scores: TokenLogprobs, *, dlogp=None, dentropy=None,
@@ -750,7 +766,6 @@ def token_logprobs_backward(ctx: Context, logits, targets, scores: TokenLogprobs
     (each may be None) with respect to ``scores``, what token_logprobs gave for these logits and targets.
     ``out`` [T, V] (the logits' type; the logits themselves are allowed) receives it."""
     T, V = _dims(logits, "logits", 2)
-    _check(logits, "logits", (BF16, F32), (T, V))
     if dentropy is not None and scores.entropy is None:
         raise ValueError("dentropy needs scores with entropy=True")
     if dtop is not None and scores.top_ids is None:
@@ -758,30 +773,30 @@ def token_logprobs_backward(ctx: Context, logits, targets, scores: TokenLogprobs
     if dlogp is not None and targets is None:
         raise ValueError("dlogp needs targets")
     top = 0 if scores.top_ids is None else _dims(scores.top_ids, "scores.top_ids", 2)[1]
-    y = _flat(ctx, targets, "targets", (I64,), (T,))
-    args = (_flat(ctx, scores.lse, "scores.lse", (F32,), (T,)), _flat(ctx, scores.entropy, "scores.entropy", (F32,), (T,)),
-            _flat(ctx, scores.top_ids, "scores.top_ids", (I64,), (T, top)), _flat(ctx, dlogp, "dlogp", (F32,), (T,)),
-            _flat(ctx, dentropy, "dentropy", (F32,), (T,)), _flat(ctx, dtop, "dtop", (F32,), (T, top)))
-    z, ld = _rows(ctx, logits, "logits", (BF16, F32), (T, V))
-    if out is None:
-        out = _new(ctx, (T, V), logits.dtype)
-    d, ldd = _rows(ctx, out, "out", (logits.dtype,), (T, V))
+    call = _Call(ctx)
+    z, ld = call.rows(logits, "logits", _FLOAT, (T, V))
+    y = call.flat(targets, "targets", _I64, (T,))
+    args = (call.flat(scores.lse, "scores.lse", _F, (T,)), call.flat(scores.entropy, "scores.entropy", _F, (T,)),
+            call.flat(scores.top_ids, "scores.top_ids", _I64, (T, top)), call.flat(dlogp, "dlogp", _F, (T,)),
+            call.flat(dentropy, "dentropy", _F, (T,)), call.flat(dtop, "dtop", _F, (T, top)))
+    out = call.new((T, V), logits.dtype) if out is None else out
+    d, ldd = call.rows(out, "out", (logits.dtype,), (T, V))
     desc = LogprobsDesc(T, V, ld, z, y, _DTYPE[logits.dtype], top)
     ctx.check(_lib.realq_token_logprobs_backward(ctx.h, ctypes.byref(desc), *args, d, ldd))
     return out
 
 
-def _attention_desc(ctx: Context, q, k, v, cu_seqlens, scale):
+def _attention_desc(call: _Call, q, k, v, cu_seqlens, scale):
     T, H, hd = _dims(q, "q", 3)
     G = _dims(k, "k", 3)[1]
     (B,) = _dims(cu_seqlens, "cu_seqlens", 1)
     if B < 1:
         raise ValueError("cu_seqlens must hold at least one offset")
-    pq, ldq = _rows(ctx, q, "q", (BF16,), (T, H, hd))
-    pk, ldk = _rows(ctx, k, "k", (BF16,), (T, G, hd))
-    pv, ldv = _rows(ctx, v, "v", (BF16,), (T, G, hd))
+    pq, ldq = call.rows(q, "q", _BF, (T, H, hd))
+    pk, ldk = call.rows(k, "k", _BF, (T, G, hd))
+    pv, ldv = call.rows(v, "v", _BF, (T, G, hd))
     return AttentionDesc(T, B - 1, H, G, hd, 0.0 if scale is None else scale,
-                         _flat(ctx, cu_seqlens, "cu_seqlens", (I32,), (B,)), pq, pk, pv, ldq, ldk, ldv)
+                         call.flat(cu_seqlens, "cu_seqlens", _I32, (B,)), pq, pk, pv, ldq, ldk, ldv)
 
 
 def packed_attention(ctx: Context, q, k, v, cu_seqlens, *, scale: Optional[float] = None, out=None):
@@ -789,11 +804,11 @@ def packed_attention(ctx: Context, q, k, v, cu_seqlens, *, scale: Optional[float
     a token in one row, rows may be strided), cu_seqlens [n_seqs + 1] int32 on the device.  Returns (out, lse):
     out like q (rows outside every sequence are left as they were), lse [n_heads, T] float32.  scale:
     1 / sqrt(head_dim) by default."""
-    desc = _attention_desc(ctx, q, k, v, cu_seqlens, scale)
-    if out is None:
-        out = _new(ctx, q.shape, BF16)
-    o, ldo = _rows(ctx, out, "out", (BF16,), q.shape)
-    lse = _new(ctx, (desc.n_heads, desc.T), F32)
+    call = _Call(ctx)
+    desc = _attention_desc(call, q, k, v, cu_seqlens, scale)
+    out = call.new(q.shape, BF16) if out is None else out
+    o, ldo = call.rows(out, "out", _BF, q.shape)
+    lse = call.new((desc.n_heads, desc.T), F32)
     ctx.check(_lib.realq_packed_attention(ctx.h, ctypes.byref(desc), o, ldo, lse.data_ptr()))
     return out, lse
 
@@ -802,17 +817,18 @@ def packed_attention_backward(ctx: Context, q, k, v, cu_seqlens, out, lse, dout,
                               dq=None, dk=None, dv=None):
     """(dq, dk, dv), bf16 like q, k and v, from what packed_attention gave and dout, the gradient at out; dk and
     dv are summed over the query heads that share them.  dq, dk, dv may be given (rows may be strided)."""
-    desc = _attention_desc(ctx, q, k, v, cu_seqlens, scale)
-    o, ldo = _rows(ctx, out, "out", (BF16,), q.shape)
-    d, lddo = _rows(ctx, dout, "dout", (BF16,), q.shape)
-    pl = _flat(ctx, lse, "lse", (F32,), (desc.n_heads, desc.T))
-    dq = _new(ctx, q.shape, BF16) if dq is None else dq
-    dk = _new(ctx, k.shape, BF16) if dk is None else dk
-    dv = _new(ctx, v.shape, BF16) if dv is None else dv
-    delta = _new(ctx, (desc.n_heads, desc.T), F32)
+    call = _Call(ctx)
+    desc = _attention_desc(call, q, k, v, cu_seqlens, scale)
+    o, ldo = call.rows(out, "out", _BF, q.shape)
+    d, lddo = call.rows(dout, "dout", _BF, q.shape)
+    pl = call.flat(lse, "lse", _F, (desc.n_heads, desc.T))
+    dq = call.new(q.shape, BF16) if dq is None else dq
+    dk = call.new(k.shape, BF16) if dk is None else dk
+    dv = call.new(v.shape, BF16) if dv is None else dv
+    delta = call.new((desc.n_heads, desc.T), F32)
     ctx.check(_lib.realq_packed_attention_backward(
-        ctx.h, ctypes.byref(desc), o, ldo, pl, d, lddo, delta.data_ptr(), *_rows(ctx, dq, "dq", (BF16,), q.shape),
-        *_rows(ctx, dk, "dk", (BF16,), k.shape), *_rows(ctx, dv, "dv", (BF16,), v.shape)))
+        ctx.h, ctypes.byref(desc), o, ldo, pl, d, lddo, delta.data_ptr(), *call.rows(dq, "dq", _BF, q.shape),
+        *call.rows(dk, "dk", _BF, k.shape), *call.rows(dv, "dv", _BF, v.shape)))
     return dq, dk, dv
 
 
@@ -820,13 +836,14 @@ def quantize_rows_i8(ctx: Context, X, out=None):
     """(codes [T, n] int8, scales [T] float32) of the rows of X [T, n] (bf16 or float32): scale max|x| / 127, codes
     to nearest even.  Codes that are not given ``out`` are laid out with rows on 16 bytes."""
     T, n = _dims(X, "X", 2)
-    x, ldx = _rows(ctx, X, "X", (BF16, F32), (T, n))
+    call = _Call(ctx)
+    x, ldx = call.rows(X, "X", _FLOAT, (T, n))
     if out is None:
-        out = _new(ctx, (T, -(-n // 16) * 16), I8)
+        out = call.new((T, -(-n // 16) * 16), I8)
         if n % 16:
             out = out[:, :n]
-    q, ldq = _rows(ctx, out, "out", (I8,), (T, n))
-    s = _new(ctx, (T,), F32)
+    q, ldq = call.rows(out, "out", _I8, (T, n))
+    s = call.new((T,), F32)
     ctx.check(_lib.realq_quantize_rows_i8(ctx.h, x, _DTYPE[X.dtype], T, n, ldx, q, ldq, s.data_ptr()))
     return out, s
 
@@ -837,14 +854,14 @@ def linear_i8(ctx: Context, Xq, sx, Wq, sw, *, bias=None, dtype=torch.bfloat16, 
     float32."""
     T, n = _dims(Xq, "Xq", 2)
     m = _dims(Wq, "Wq", 2)[0]
-    x, ldx = _rows(ctx, Xq, "Xq", (I8,), (T, n))
-    w, ldw = _rows(ctx, Wq, "Wq", (I8,), (m, n))
+    call = _Call(ctx)
+    x, ldx = call.rows(Xq, "Xq", _I8, (T, n))
+    w, ldw = call.rows(Wq, "Wq", _I8, (m, n))
     if out is None:
         if dtype not in _DTYPE:
             raise ValueError(f"dtype must be torch.bfloat16 or torch.float32, got {dtype}")
-        out = _new(ctx, (T, m), dtype)
-    y, ldy = _rows(ctx, out, "out", (BF16, F32), (T, m))
-    ctx.check(_lib.realq_linear_i8(ctx.h, x, ldx, _flat(ctx, sx, "sx", (F32,), (T,)), w, ldw,
-                                   _flat(ctx, sw, "sw", (F32,), (m,)), _flat(ctx, bias, "bias", (F32,), (m,)), T, n, m,
-                                   y, _DTYPE[out.dtype], ldy))
+        out = call.new((T, m), dtype)
+    y, ldy = call.rows(out, "out", _FLOAT, (T, m))
+    ctx.check(_lib.realq_linear_i8(ctx.h, x, ldx, call.flat(sx, "sx", _F, (T,)), w, ldw, call.flat(sw, "sw", _F, (m,)),
+                                   call.flat(bias, "bias", _F, (m,)), T, n, m, y, _DTYPE[out.dtype], ldy))
     return out

@@ -64,21 +64,19 @@ def test_binding_structs_match_the_c_layout(tmp_path):
             assert got[(cname, f)] == getattr(py, f).offset, (cname, f)
 
 
-def test_binding_refuses_before_the_call():
+def test_binding_refuses_before_the_call(monkeypatch):
     import torch
     from paper_2609_00049_amd import realq as rq
 
-    class Stream:
-        device = torch.device("cuda:0")
-        cuda_stream = 0
-
     class NoCall:
         h = None
-        stream = Stream()
+        device = torch.device("cuda:0")
+        raw_stream = 0
 
         def check(self, rc):
             raise AssertionError("the C ABI was called")
 
+    monkeypatch.setattr(rq, "_current", lambda i: 0)
     ctx = NoCall()
     z, y = torch.zeros((4, 50)), torch.zeros(4, dtype=torch.int64)
     s = rq.TokenLogprobs(torch.zeros(4), torch.zeros(4), None, None, None)
