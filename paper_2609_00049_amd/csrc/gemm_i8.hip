@@ -19,20 +19,21 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 
-// The whole number nearest x / s, ties to even, for |x| <= 127.5 s or so: the float32 quotient's rounding can
-// fall on the wrong side of a half, and the remainder r = x - q s, exact by one fused multiply-add, says so.
-// Operands below the normal range of products are raised by a power of two first (both: exact).
+// The whole number nearest x / s, ties to even: the float32 quotient's rounding can fall on the wrong side of
+// a half, and the remainder r = x - q s, exact by one fused multiply-add, says so.
+__device__ __forceinline__ float nearer(float q, float r, float h) {
+    const bool odd = ((int)q & 1) != 0;
+    return fabsf(r) > h || (fabsf(r) == h && odd) ? q + copysignf(1.f, r) : q;
+}
+// For any s > 0: operands below the normal range of products are raised by a power of two first (both:
+// exact), and a subnormal s can be so much too small that the code is cut.
 __device__ __forceinline__ float code_of(float x, float s) {
     if (s < 0x1p-100f) {
         x *= 0x1p120f;
         s *= 0x1p120f;
     }
-    float q = rintf(x / s);
-    const float r = fmaf(-q, s, x), h = 0.5f * s;
-    const bool odd = ((int)q & 1) != 0;
-    if (r > h || (r == h && odd)) q += 1.f;
-    else if (r < -h || (r == -h && odd)) q -= 1.f;
-    return fminf(fmaxf(q, -127.f), 127.f);
+    const float q = rintf(x / s);
+    return fminf(fmaxf(nearer(q, fmaf(-q, s, x), 0.5f * s), -127.f), 127.f);
 }
 
 // y[0..count) to p, `wide`: p is aligned to 4 elements
@@ -60,29 +61,129 @@ constexpr int QT = 256;
 
 }  // namespace
 
+namespace {
+
+// the bits of |x| keep its order, infinities and NaN above all finite values
+__device__ __forceinline__ uint32_t size_of(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+__device__ __forceinline__ float scale_of(uint32_t most) {
+    return most < 0x7F800000u ? __uint_as_float(most) / 127.f : NAN;
+}
 template <class E>
-__global__ __launch_bounds__(QT) void quantize_rows_kernel(const E* __restrict__ X, int64_t T, int64_t n, int64_t ldx,
-                                                           int8_t* __restrict__ Q, int64_t ldq,
-                                                           float* __restrict__ S) {
+__device__ __forceinline__ float as_float(E x) {
+    if constexpr (sizeof(E) == 2) return bf2f(x);
+    else return x;
+}
+
+}  // namespace
+
+// Any strides, alignment and length: two reads of the row, an element a thread.
+template <class E>
+__global__ __launch_bounds__(QT) void quantize_any_kernel(const E* __restrict__ X, int64_t T, int64_t n, int64_t ldx,
+                                                          int8_t* __restrict__ Q, int64_t ldq,
+                                                          float* __restrict__ S) {
     __shared__ uint32_t red[QT / 64];
     for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
         const E* x = X + t * ldx;
-        auto at = [&](int64_t j) {
-            if constexpr (sizeof(E) == 2) return bf2f(x[j]);
-            else return x[j];
-        };
-        // the bits of |x| keep its order, infinities and NaN above all finite values
         uint32_t m = 0;
-        for (int64_t j = threadIdx.x; j < n; j += QT) m = max(m, __float_as_uint(at(j)) & 0x7FFFFFFFu);
+        for (int64_t j = threadIdx.x; j < n; j += QT) m = max(m, size_of(as_float(x[j])));
         for (int w = 32; w > 0; w >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w));
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
         __syncthreads();
         for (int w = 0; w < QT / 64; ++w) m = max(m, red[w]);
-        const bool finite = m < 0x7F800000u;
-        const float s = finite ? __uint_as_float(m) / 127.f : NAN;
+        const float s = scale_of(m);
         if (threadIdx.x == 0) S[t] = s;
-        for (int64_t j = threadIdx.x; j < n; j += QT) Q[t * ldq + j] = (int8_t)(s > 0.f ? (int)code_of(at(j), s) : 0);
+        for (int64_t j = threadIdx.x; j < n; j += QT)
+            Q[t * ldq + j] = (int8_t)(s > 0.f ? (int)code_of(as_float(x[j]), s) : 0);
         __syncthreads();
+    }
+}
+
+// Rows on 16 bytes of at most 8 PER threads-per-row elements, held in registers between the maximum and the
+// codes: one read of X, one write of Q.  RT threads a row (a wave, or a whole block).
+template <class E, int RT, int PER>
+__global__ __launch_bounds__(RT < QT ? QT : RT) void quantize_rows_kernel(const E* __restrict__ X, int64_t T,
+                                                                          int64_t n, int64_t ldx,
+                                                                          int8_t* __restrict__ Q, int64_t ldq,
+                                                                          float* __restrict__ S) {
+    constexpr int NT = RT < QT ? QT : RT, RPB = NT / RT;
+    __shared__ uint32_t red[NT / 64];
+    const int tid = threadIdx.x % RT;
+    for (int64_t t0 = (int64_t)blockIdx.x * RPB; t0 < T; t0 += (int64_t)gridDim.x * RPB) {
+        const int64_t t = t0 + threadIdx.x / RT;
+        const bool row = t < T;
+        const E* x = X + t * ldx;
+        float f[PER][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int64_t j = ((int64_t)p * RT + tid) * 8;
+            if (row && j + 8 <= n) {
+                if constexpr (sizeof(E) == 2) {
+                    const u16x8 v = *reinterpret_cast<const u16x8*>(x + j);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[p][e] = bf2f(v[e]);
+                } else {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(x + j), w = *reinterpret_cast<const f32x4*>(x + j + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[p][e] = e < 4 ? v[e] : w[e - 4];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[p][e] = row && j + e < n ? as_float(x[j + e]) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = max(m, size_of(f[p][e]));
+        }
+        for (int w = 32; w > 0; w >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, w));
+        if constexpr (RT > 64) {
+            if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < NT / 64; ++w) m = max(m, red[w]);
+            __syncthreads();
+        }
+        const float s = scale_of(m);
+        if (!row) continue;
+        if (tid == 0) S[t] = s;
+        const bool plain = s >= 0x1p-100f;  // false for 0 and NaN too
+        const float inv = plain ? 1.f / s : 0.f, h = 0.5f * s;
+        int8_t* q = Q + t * ldq;
+#pragma unroll
+        for (int p = 0; p < PER; ++p) {
+            const int64_t j = ((int64_t)p * RT + tid) * 8;
+            if (j >= n) break;
+            int c[8];
+            if (plain) {
+                // the product with 1 / s is within 2 roundings of the quotient: the nearest whole number of it is
+                // the code, unless it lies at the half between two, which the remainder shows
+                float k[8];
+                bool edge = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    k[e] = rintf(f[p][e] * inv);
+                    edge |= fabsf(fmaf(-k[e], s, f[p][e])) >= h;
+                }
+                if (edge)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) k[e] = nearer(k[e], fmaf(-k[e], s, f[p][e]), h);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) c[e] = (int)k[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) c[e] = s > 0.f ? (int)code_of(f[p][e], s) : 0;
+            }
+            u32x2 v;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                v[e] = (uint32_t)(c[4 * e] & 255) | (uint32_t)(c[4 * e + 1] & 255) << 8 |
+                       (uint32_t)(c[4 * e + 2] & 255) << 16 | (uint32_t)c[4 * e + 3] << 24;
+            if (j + 8 <= n) {
+                *reinterpret_cast<u32x2*>(q + j) = v;
+            } else {
+                for (int e = 0; e < 8; ++e)
+                    if (j + e < n) q[j + e] = (int8_t)(v[e >> 2] >> (8 * (e & 3)));
+            }
+        }
     }
 }
 
@@ -190,25 +291,25 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64
 
 }  // namespace
 
-template <int WM, int WN, class E>
+template <int WM, int WN, int SM, int SN, int NS, class E>
 __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
     const int8_t* __restrict__ W, int64_t ldw, const int8_t* __restrict__ X, int64_t ldx, int64_t m, int64_t T,
     int64_t n, const float* __restrict__ sx, const float* __restrict__ sw, const float* __restrict__ bias,
     E* __restrict__ Y, int64_t ldy, int64_t tm, int64_t tn, int64_t band) {
-    constexpr int BM = 64 * WM, BN = 128 * WN, NW = WM * WN, NT = 64 * NW;
+    constexpr int BM = 32 * SM * WM, BN = 32 * SN * WN, NW = WM * WN, NT = 64 * NW, STAGE = (BM + BN) * SL;
     constexpr int RA = BM / 16 / NW, RB = BN / 16 / NW;  // 1 KB runs (16 rows) a wave loads of each operand
-    __shared__ __attribute__((aligned(16))) int8_t st0[(BM + BN) * SL], st1[(BM + BN) * SL], st2[(BM + BN) * SL];
+    __shared__ __attribute__((aligned(16))) int8_t stages[NS * STAGE];
     __shared__ __attribute__((aligned(16))) float rows[2 * BM];  // the tile's output scales and biases
     int64_t ti, tj;
     tile_of(blockIdx.x, tm, tn, band, ti, tj);
     const int64_t i0 = ti * BM, t0 = tj * BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / WN * 64, wn = wave % WN * 128;
-    i32x16 acc[2][4];
+    const int wm = wave / WN * (32 * SM), wn = wave % WN * (32 * SN);
+    i32x16 acc[SM][SN];
 #pragma unroll
-    for (int a = 0; a < 2; ++a)
+    for (int a = 0; a < SM; ++a)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < SN; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
     // each lane's source offsets; rows past the end read the last one, into results that are not stored
@@ -226,8 +327,9 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
     }
     const int8_t* const bw = W + i0 * ldw;
     const int8_t* const bx = X + t0 * ldx;
-    const uint32_t at[3] = {lds_at(st0), lds_at(st1), lds_at(st2)};
-    auto issue = [&](int64_t s, uint32_t stage) {
+    const uint32_t base = lds_at(stages);
+    auto issue = [&](int64_t s, int st) {
+        const uint32_t stage = base + st * STAGE;
 #pragma unroll
         for (int q = 0; q < RA; ++q) to_lds(bw + s * SL, oa[q], stage + (wave + NW * q) * 1024);
 #pragma unroll
@@ -239,16 +341,16 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
     auto multiply = [&](const int8_t* st) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            i32x4 a[2], b[4];
+            i32x4 a[SM], b[SN];
             const int c = 2 * k + (lane >> 5);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) a[i] = frag(st, wm + 32 * i + (lane & 31), c);
+            for (int i = 0; i < SM; ++i) a[i] = frag(st, wm + 32 * i + (lane & 31), c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
+            for (int j = 0; j < SN; ++j) b[j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < SM; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < SN; ++j)
                     acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
         }
     };
@@ -273,10 +375,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
                     if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[e] << (8 * (e & 3)));
             }
             const int rr = w ? r : r - BM;
-            *reinterpret_cast<i32x4*>(st0 + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
+            *reinterpret_cast<i32x4*>(stages + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
         }
         __syncthreads();
-        multiply(st0);
+        multiply(stages);
         __syncthreads();
     }
     if constexpr (NW == 8) {
@@ -285,23 +387,24 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
         // work while a wave waits for LDS: group 1 enters the loop one barrier later.  Slice s lies in stage
         // s % 3; a wave loads its part of slice s + 2 into the stage of slice s - 1, which both groups have
         // read, and waits until its part of slice s + 1 has landed, before either group reads that.
+        static_assert(NS == 3, "the ping-pong rotates three stages");
         const int group = wave >> 2;
-        auto fetch = [&](int64_t s, const int8_t* st, uint32_t refill, i32x4 (&a)[2][2], i32x4 (&b)[2][4]) {
+        auto fetch = [&](int64_t s, const int8_t* st, int refill, i32x4 (&a)[2][SM], i32x4 (&b)[2][SN]) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int c = 2 * k + (lane >> 5);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) a[k][i] = frag(st, wm + 32 * i + (lane & 31), c);
+                for (int i = 0; i < SM; ++i) a[k][i] = frag(st, wm + 32 * i + (lane & 31), c);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) b[k][j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
+                for (int j = 0; j < SN; ++j) b[k][j] = frag(st + BM * SL, wn + 32 * j + (lane & 31), c);
             }
             if (s + 2 < full) issue(s + 2, refill);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             if (s + 2 < full) vm_wait<RA + RB>();
             else vm_wait<0>();
         };
-        auto slice = [&](int64_t s, const int8_t* st, uint32_t refill) {
-            i32x4 a[2][2], b[2][4];
+        auto slice = [&](int64_t s, const int8_t* st, int refill) {
+            i32x4 a[2][SM], b[2][SN];
             fetch(s, st, refill, a, b);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_barrier();
@@ -309,62 +412,59 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < SM; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < SN; ++j)
                         acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[k][i], b[k][j], acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        if (full > 0) issue(0, at[0]);
-        if (full > 1) issue(1, at[1]);
+        if (full > 0) issue(0, 0);
+        if (full > 1) issue(1, 1);
         if (full > 1) vm_wait<RA + RB>();
         else vm_wait<0>();
         __builtin_amdgcn_s_barrier();
         if (group == 1) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         for (int64_t s = 0; s < full; s += 3) {
-            slice(s, st0, at[2]);
+            slice(s, stages, 2);
             if (s + 1 >= full) break;
-            slice(s + 1, st1, at[0]);
+            slice(s + 1, stages + STAGE, 0);
             if (s + 2 >= full) break;
-            slice(s + 2, st2, at[1]);
+            slice(s + 2, stages + 2 * STAGE, 1);
         }
         if (group == 0) __builtin_amdgcn_s_barrier();
     } else {
-        // slice s: its loads have landed, everyone's are visible and nobody reads the stage of slice s - 1 any more
-        auto step = [&](int64_t s, const int8_t* st, uint32_t refill) {
-            if (s + 1 < full) vm_wait<RA + RB>();
+        // slice s: its loads have landed, everyone's are visible and nobody reads the stage of slice s - 1 any
+        // more; NS - 1 slices are under way, so a slice waits for memory once in NS - 1
+        for (int s = 0; s < NS - 1; ++s)
+            if (s < full) issue(s, s);
+        int st = 0;
+        for (int64_t s = 0; s < full; ++s) {
+            if (s + NS - 2 < full) vm_wait<(NS - 2) * (RA + RB)>();
             else vm_wait<0>();
             __builtin_amdgcn_s_barrier();
-            if (s + 2 < full) issue(s + 2, refill);
-            multiply(st);
-        };
-        if (full > 0) issue(0, at[0]);
-        if (full > 1) issue(1, at[1]);
-        for (int64_t s = 0; s < full; s += 3) {
-            step(s, st0, at[2]);
-            if (s + 1 >= full) break;
-            step(s + 1, st1, at[0]);
-            if (s + 2 >= full) break;
-            step(s + 2, st2, at[1]);
+            const int before = st == 0 ? NS - 1 : st - 1;
+            if (s + NS - 1 < full) issue(s + NS - 1, before);
+            multiply(stages + st * STAGE);
+            st = st + 1 == NS ? 0 : st + 1;
         }
     }
-    // The wave's 64 outputs of 32 tokens at a time, through LDS of its own so that the stores are whole lines:
-    // a lane holds one token and 4 consecutive outputs, and stores 16 bytes of a token's 64 outputs.
-    constexpr int PER = 16 / (int)sizeof(E), LPR = 64 / PER, ROW = 64 + PER;  // lanes per token, elements per LDS row
-    static_assert((NW + 2) / 3 * 32 * ROW * (int)sizeof(E) <= (BM + BN) * SL, "the stages hold the outputs");
+    // The wave's 32 SM outputs of 32 tokens at a time, through LDS of its own so that the stores are whole lines:
+    // a lane holds one token and 4 consecutive outputs, and stores 16 bytes of a token's outputs.
+    constexpr int OUT = 32 * SM, PER = 16 / (int)sizeof(E), LPR = OUT / PER, ROW = OUT + PER;  // lanes a token, LDS row
+    static_assert(NW * 32 * ROW * (int)sizeof(E) <= NS * STAGE, "the stages hold the outputs");
     __syncthreads();
-    E* const own = reinterpret_cast<E*>(wave % 3 == 0 ? st0 : wave % 3 == 1 ? st1 : st2) + wave / 3 * (32 * ROW);
+    E* const own = reinterpret_cast<E*>(stages) + wave * (32 * ROW);
     const bool wide = ldy % PER == 0 && ((uintptr_t)Y & 15) == 0;
     const int64_t r0 = i0 + wm;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < SN; ++j) {
         const int64_t tb = t0 + wn + 32 * j;
         const float st = sx[min(tb + (lane & 31), T - 1)];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < SM; ++i)
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
                 const int c = 32 * i + 8 * (e >> 2) + 4 * (lane >> 5);
@@ -380,7 +480,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
                 put4(own + (lane & 31) * ROW + c, y, true, 4);
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (wide && r0 + 64 <= m) {
+        if (wide && r0 + OUT <= m) {
             const int c = lane % LPR * PER;
 #pragma unroll
             for (int q = 0; q < LPR / 2; ++q) {
@@ -390,23 +490,132 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
             }
         } else {  // an output a lane
             const int rows_here = (int)min(T - tb, (int64_t)32);
-            if (r0 + lane < m)
-                for (int row = 0; row < rows_here; ++row) Y[(tb + row) * ldy + r0 + lane] = own[row * ROW + lane];
+            const int c = lane % OUT;
+            if (r0 + c < m)
+                for (int row = lane / OUT; row < rows_here; row += 64 / OUT) Y[(tb + row) * ldy + r0 + c] = own[row * ROW + c];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
+// ---------------------------------------------------------------- few tokens: the weights are read once
+// A block takes 16 weight rows and its waves a share of the columns each, 128 at a time (a row's whole line),
+// straight from memory into the operand layout of v_mfma_i32_16x16x64_i8: lane l holds 16 columns of row
+// l % 16, and of token l % 16.  The waves' integer sums meet in LDS.
+template <int TT, class E>
+__global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __restrict__ W, int64_t ldw,
+                                                            const int8_t* __restrict__ X, int64_t ldx, int64_t m,
+                                                            int64_t T, int64_t n, const float* __restrict__ sx,
+                                                            const float* __restrict__ sw,
+                                                            const float* __restrict__ bias, E* __restrict__ Y,
+                                                            int64_t ldy) {
+    constexpr int NW = 8, U = TT <= 2 ? 4 : 2;  // steps of 128 columns under way in a wave
+    __shared__ int32_t part[NW][TT * 256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i0 = (int64_t)blockIdx.x * 16;
+    const int8_t* w = W + min(i0 + (lane & 15), m - 1) * ldw;
+    const int8_t* x[TT];
+    bool here[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        here[t] = 16 * t + (lane & 15) < T;
+        x[t] = X + (here[t] ? 16 * t + (lane & 15) : 0) * ldx;
+    }
+    auto load = [&](const int8_t* p, int64_t k) {
+        i32x4 v = {0, 0, 0, 0};
+        if (k + 16 <= n) {
+            v = *reinterpret_cast<const i32x4*>(p + k);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[k + e] << (8 * (e & 3)));
+        }
+        return v;
+    };
+    i32x4 acc[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+    const int64_t steps = (n + 127) / 128;
+    // lanes l / 16 = 0..3 hold the 32-column quarters of a step: 16 columns for each of two products
+    const int64_t kl = 32 * (lane >> 4);
+    int64_t s = wave;
+    for (; s + (U - 1) * NW < steps && (s + (U - 1) * NW + 1) * 128 <= n; s += U * NW) {
+        i32x4 a[U][2], b[U][2][TT];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t k = (s + u * NW) * 128 + kl + 16 * h;
+                a[u][h] = *reinterpret_cast<const i32x4*>(w + k);
+#pragma unroll
+                for (int t = 0; t < TT; ++t) {
+                    b[u][h][t] = i32x4{0, 0, 0, 0};
+                    if (here[t]) b[u][h][t] = *reinterpret_cast<const i32x4*>(x[t] + k);
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < TT; ++t)
+                    acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][h], b[u][h][t], acc[t], 0, 0, 0);
+    }
+    for (; s < steps; s += NW)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t k = s * 128 + kl + 16 * h;
+            const i32x4 a = load(w, k);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const i32x4 b = here[t] ? load(x[t], k) : i32x4{0, 0, 0, 0};
+                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc[t], 0, 0, 0);
+            }
+        }
+    // register e of a 16 x 16 result: row 4 (lane / 16) + e, token lane % 16
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[wave][t * 256 + (lane & 15) * 16 + 4 * (lane >> 4) + e] = acc[t][e];
+    __syncthreads();
+    for (int o = threadIdx.x; o < TT * 256; o += NW * 64) {
+        const int64_t t = o >> 4, i = i0 + (o & 15);
+        if (t >= T || i >= m) continue;
+        int32_t v = 0;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) v += part[k][o];
+        float y = (float)v * sx[t] * sw[i];
+        if (bias) y += bias[i];
+        if constexpr (sizeof(E) == 2) Y[t * ldy + i] = __builtin_bit_cast(uint16_t, (__bf16)y);
+        else Y[t * ldy + i] = y;
+    }
+}
+
+namespace {
+
+template <class E>
+hipError_t quantize(const E* X, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq, float* s, hipStream_t st) {
+    const bool on16 = ((uintptr_t)X & 15) == 0 && ldx * (int64_t)sizeof(E) % 16 == 0 && ((uintptr_t)Q & 7) == 0 && ldq % 8 == 0;
+    const unsigned rows = (unsigned)std::min<int64_t>(T, 1 << 20), quads = (unsigned)std::min<int64_t>((T + 3) / 4, 1 << 20);
+#define RQ_ROWS(RT, PER, GRID)                                                                                      \
+    hipLaunchKernelGGL((quantize_rows_kernel<E, RT, PER>), dim3(GRID), dim3(RT < QT ? QT : RT), 0, st, X, T, n, ldx, \
+                       Q, ldq, s)
+    if (!on16 || n > 16384) hipLaunchKernelGGL(quantize_any_kernel<E>, dim3(rows), dim3(QT), 0, st, X, T, n, ldx, Q, ldq, s);
+    else if (n <= 512) RQ_ROWS(64, 1, quads);
+    else if (n <= 2048) RQ_ROWS(64, 4, quads);
+    else if (n <= 4096) RQ_ROWS(256, 2, rows);
+    else if (n <= 8192) RQ_ROWS(256, 4, rows);
+    else RQ_ROWS(512, 4, rows);
+#undef RQ_ROWS
+    return hipGetLastError();
+}
+
+}  // namespace
+
 hipError_t quantize_rows_i8(const void* X, bool f32, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq,
                             float* s, hipStream_t st) {
-    const dim3 grid((unsigned)std::min<int64_t>(T, 1 << 20));
-    if (f32)
-        hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, dim3(QT), 0, st, (const float*)X, T, n, ldx, Q,
-                           ldq, s);
-    else
-        hipLaunchKernelGGL(quantize_rows_kernel<uint16_t>, grid, dim3(QT), 0, st, (const uint16_t*)X, T, n,
-                           ldx, Q, ldq, s);
-    return hipGetLastError();
+    return f32 ? quantize((const float*)X, T, n, ldx, Q, ldq, s, st)
+               : quantize((const uint16_t*)X, T, n, ldx, Q, ldq, s, st);
 }
 
 namespace {
@@ -419,25 +628,41 @@ hipError_t simple(const LinearI8Args& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int WM, int WN, class E>
+template <int WM, int WN, int SM, int SN, int NS, class E>
 hipError_t tiled(const LinearI8Args& a, hipStream_t st) {
-    const int64_t tm = (a.m + 64 * WM - 1) / (64 * WM), tn = (a.T + 128 * WN - 1) / (128 * WN);
-    const char* be = getenv("RQ_BAND");
-    const int64_t band = be ? atoi(be) : 8;
-    hipLaunchKernelGGL((linear_i8_tile_kernel<WM, WN, E>), dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0, st, a.W,
-                       a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy, tm, tn, band);
+    constexpr int BM = 32 * SM * WM, BN = 32 * SN * WN;
+    const int64_t tm = (a.m + BM - 1) / BM, tn = (a.T + BN - 1) / BN;
+    hipLaunchKernelGGL((linear_i8_tile_kernel<WM, WN, SM, SN, NS, E>), dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0,
+                       st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy, tm, tn, 8);
+    return hipGetLastError();
+}
+
+template <class E>
+hipError_t few(const LinearI8Args& a, hipStream_t st) {
+    const dim3 grid((unsigned)((a.m + 15) / 16));
+#define RQ_FEW(TT)                                                                                                    \
+    hipLaunchKernelGGL((linear_i8_few_kernel<TT, E>), grid, dim3(512), 0, st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, \
+                       a.sx, a.sw, a.bias, (E*)a.Y, a.ldy)
+    if (a.T <= 16) RQ_FEW(1);
+    else if (a.T <= 32) RQ_FEW(2);
+    else RQ_FEW(4);
+#undef RQ_FEW
     return hipGetLastError();
 }
 
 template <class E>
 hipError_t linear(const LinearI8Args& a, hipStream_t st) {
     const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && a.ldx % 16 == 0 && a.ldw % 16 == 0;
-    const char* v = getenv("RQ_TILE");
-    const int k = v ? atoi(v) : 1;
-    if (!on16 || a.T <= 64 || k == 0) return simple<E>(a, st);
-    if (k == 1) return tiled<2, 2, E>(a, st);
-    if (k == 2) return tiled<4, 2, E>(a, st);
-    return tiled<2, 1, E>(a, st);
+    if (!on16 || a.ldw >= (1 << 22) || a.ldx >= (1 << 22)) return simple<E>(a, st);  // 32-bit offsets in a tile
+    // Few tokens: past 16 of them the weights' rows in 64 x 64 tiles, if there are enough for half the CUs
+    // (24 tokens, 4096 x 14336: 17 us against 27 us), else the kernel that splits the columns over waves
+    // (14336 x 4096: 21 us against 44 us; one token, 4096 x 14336: 15 us against 16 us).
+    if (a.T <= 64 && (a.T <= 16 ? a.m <= 1 << 22 : a.m < 8192)) return few<E>(a, st);
+    // 256 x 256 tiles where they fill a quarter of the 256 CUs (1024 x 4096 x 4096, 64 tiles: 40 us against 51 us;
+    // 2048 x 5120 x 5120: 63 us against 125 us), else 64 x 64 (512 x 4096 x 4096: 20 us against 40 us).
+    const int64_t large = ((a.m + 255) / 256) * ((a.T + 255) / 256);
+    if (large < 64) return tiled<2, 2, 1, 1, 6, E>(a, st);
+    return tiled<4, 2, 2, 4, 3, E>(a, st);
 }
 
 }  // namespace
