@@ -609,7 +609,8 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  * (rows of one wider array are fine).
  *
  * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
- * 128, 256); every array on 16 bytes and every row stride a multiple of 8.  q, k, v and dO must be
+ * 128, 256); every array on 16 bytes and every row stride a multiple of 8, at most 2^24;
+ * (T / 128 + n_seqs) n_heads <= 2^23.  q, k, v and dO must be
  * finite: a NaN or an infinity can reach every row of its own sequence, and no other sequence.  Offsets that
  * decrease or leave 0 .. T are cut to the arrays, with results of no meaning. */
 typedef struct realq_attention_desc {

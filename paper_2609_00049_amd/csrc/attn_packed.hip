@@ -121,6 +121,70 @@ __device__ __forceinline__ Seq find_tile(const int32_t* __restrict__ cu, int64_t
     return s;
 }
 
+// Lane i fills LDS bytes lds + 16 i .. + 15 from base + its own byte offset; completion is waited for by
+// vm_wait, not by the compiler.
+__device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void block_sync() {  // LDS written by to_lds is visible once its writers have waited
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)p; }
+
+// Brings rows r0 .. r0 + ROWS - 1 of one head (past the sequence's last one: that one again) into an LDS
+// tile by direct-to-LDS loads, NW waves sharing the work.  Channels from hd on are not touched: the tile is
+// cleared once, and a chunk's place depends on its row modulo 16 only.
+template <int HD, int ROWS, int NW>
+struct Loader {
+    static constexpr int CH = HD / 8, RPI = 64 / CH, STEP = RPI * NW, N = ROWS / STEP;  // rows an instruction; loads
+    static constexpr int D = STEP % 16 ? 16 / STEP : 1;  // distinct chunk patterns
+    static_assert(ROWS % STEP == 0 && (STEP % 16 == 0 || 16 % STEP == 0), "whole instructions");
+    int row, wave;
+    uint32_t chunk[D];  // byte offset of this lane's chunk in its row
+    bool on[D];
+    __device__ Loader(int hd) {
+        const int lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        row = wave * RPI + lane / CH;
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int c = (lane % CH) ^ swz<HD>(row + d * STEP);
+            chunk[d] = c * 16;
+            on[d] = c * 8 < hd;
+        }
+    }
+    __device__ void load(const uint16_t* __restrict__ g, int64_t ld, int r0, int len, uint32_t lds) const {
+        const uint16_t* base = g + (int64_t)r0 * ld;
+        const uint32_t pitch = (uint32_t)(2 * ld);
+        if (r0 + ROWS <= len) {
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                if (on[q % D])
+                    to_lds(base + (int64_t)(q * STEP) * ld, row * pitch + chunk[q % D], lds + (wave + NW * q) * 1024);
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                if (on[q % D])
+                    to_lds(base, (uint32_t)min(row + q * STEP, len - 1 - r0) * pitch + chunk[q % D],
+                           lds + (wave + NW * q) * 1024);
+        }
+    }
+};
+// Zeros in the channels from hd on of a tile.
+template <int HD, int ROWS, int NT>
+__device__ __forceinline__ void clear_rest(uint16_t* lds, int hd) {
+    if (hd == HD) return;
+    for (int i = threadIdx.x; i < ROWS * HD / 8; i += NT)
+        *reinterpret_cast<u16x8*>(lds + i * 8) = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    __syncthreads();
+}
+
 // rows r0 .. r0 + ROWS - 1 (past the last one: the last one again) of one head into an LDS tile
 template <int HD, int ROWS, int NT>
 __device__ __forceinline__ void stage(const uint16_t* __restrict__ g, int64_t ld, int hd, int r0, int len,
@@ -150,64 +214,99 @@ constexpr int NT = 256, BM = 128;
 
 }  // namespace
 
+// This block's item: each XCD (blocks are dealt to the 8 round-robin) takes a run of consecutive heads, whose
+// keys and values its L2 then holds; within a head the last tiles, which see the most keys, come first.
+__device__ __forceinline__ void item_of(int64_t tiles, int64_t& slot, int& head) {
+    const int64_t n = gridDim.x, q = n >> 3, r = n & 7, x = blockIdx.x & 7;
+    const int64_t L = x * q + min(x, r) + (blockIdx.x >> 3);
+    head = (int)(L / tiles);
+    slot = tiles - 1 - L % tiles;
+}
+
+// O and lse of 128 queries, 32 a wave, over 64-key tiles in two LDS buffers (the next tile is loaded while
+// one is used).  S^T = K Q^T leaves a query's scores in one lane, O^T = V^T P^T its outputs, so the running
+// maximum, sum and rescaling are the lane's own; only the maximum and the final sum cross to lane + 32.
+// O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
+// old one serves as well (P up to 256, exact to the same relative rounding).
 template <int HD>
-__global__ __launch_bounds__(NT) void attn_forward_kernel(AttnArgs a, uint16_t* __restrict__ O, int64_t ldo,
-                                                          float* __restrict__ lse) {
-    constexpr int BN = 64;
-    __shared__ __attribute__((aligned(16))) uint16_t sk[BN * HD], sv[BN * HD];
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+__global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a, uint16_t* __restrict__ O,
+                                                                             int64_t ldo, float* __restrict__ lse,
+                                                                             int64_t tiles) {
+    constexpr int BN = HD <= 128 ? 64 : 32, NB = BN / 32;
+    __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
+    int64_t slot;
+    int h;
+    item_of(tiles, slot, h);
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
     if (!sq.any) return;
-    const int h = blockIdx.y, kv = h / (a.n_heads / a.n_kv);
+    const int kv = h / (a.n_heads / a.n_kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int q0 = sq.tile * BM + wave * 32;          // this wave's first query, in the sequence
+    const int q0 = sq.tile * BM + wave * 32;           // this wave's first query, in the sequence
     const int qi = min(q0 + (lane & 31), sq.len - 1);  // this lane's
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
+    clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
+    const Loader<HD, BN, NT / 64> loader(a.hd);
+    const int keys = min((sq.tile + 1) * BM, sq.len);
+    loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
+    loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
     bf16x8 qf[HD / 16];
     hold<HD>(a.q + (sq.begin + qi) * a.ldq + h * a.hd, a.hd, lane, qf);
     const float c = a.scale * kLog2e;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY, mc = 0.f, l = 0.f;
     f32x16 o[HD / 32];
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) o[t] = zero16();
-    const int keys = min((sq.tile + 1) * BM, sq.len);
-    for (int k0 = 0; k0 < keys; k0 += BN) {
-        __syncthreads();
-        stage<HD, BN, NT>(K, a.ldk, a.hd, k0, sq.len, sk);
-        stage<HD, BN, NT>(V, a.ldv, a.hd, k0, sq.len, sv);
-        __syncthreads();
+    int buf = 0;
+    for (int k0 = 0; k0 < keys; k0 += BN, buf ^= 1) {
+        vm_wait<0>();
+        block_sync();
+        if (k0 + BN < keys) {
+            loader.load(K, a.ldk, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][0]));
+            loader.load(V, a.ldv, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][1]));
+        }
         if (k0 > q0 + 31) continue;
-        f32x16 s[2] = {zero16(), zero16()};
+        const uint16_t* sk = kv_lds[buf][0];
+        const uint16_t* sv = kv_lds[buf][1];
+        f32x16 s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = zero16();
 #pragma unroll
         for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) s[b] = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s[b]);
-        float mx = -INFINITY;
+            for (int b = 0; b < NB; ++b) s[b] = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s[b]);
+        if (k0 + BN - 1 > q0)  // a tile that some query of the wave sees in part
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if (k0 + 32 * b + crow(e, lane) > qi) s[b][e] = -INFINITY;
-                mx = fmaxf(mx, s[b][e]);
-            }
+                for (int e = 0; e < 16; ++e)
+                    if (k0 + 32 * b + crow(e, lane) > qi) s[b][e] = -INFINITY;
+        float mx = s[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
         mx = fmaxf(mx, other_half(mx));
-        const float mn = fmaxf(m, mx);
-        const float f = __builtin_amdgcn_exp2f((m - mn) * c);
-        m = mn;
-        l *= f;
+        if (__any((mx - m) * c > 8.f)) {  // the first tile too: m is -infinity
+            const float mn = fmaxf(m, mx);
+            const float f = __builtin_amdgcn_exp2f((m - mn) * c);
+            m = mn;
+            mc = m * c;
+            l *= f;
 #pragma unroll
-        for (int t = 0; t < HD / 32; ++t)
+            for (int t = 0; t < HD / 32; ++t)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[t][e] *= f;
+                for (int e = 0; e < 16; ++e) o[t][e] *= f;
+        }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f((s[b][e] - m) * c);
+                s[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], c, -mc));
                 l += s[b][e];
             }
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const bf16x8 p = pack_frag(s[b], x);
@@ -391,8 +490,9 @@ __global__ __launch_bounds__(NT) void attn_dkv_kernel(AttnArgs a, const float* _
     } while (0)
 
 hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st) {
-    const dim3 grid((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_heads);
-    RQ_HEAD_DIM(attn_forward_kernel, grid, a, O, ldo, lse);
+    const int64_t tiles = a.T / BM + a.n_seqs;
+    const dim3 grid((unsigned)(tiles * a.n_heads));
+    RQ_HEAD_DIM(attn_forward_kernel, grid, a, O, ldo, lse, tiles);
     return hipGetLastError();
 }
 

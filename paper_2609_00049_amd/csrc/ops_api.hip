@@ -74,6 +74,8 @@ int check_attention(realq_ctx* ctx, const realq_attention_desc* d, const char* w
         return set_error(ctx, REALQ_ERR_SHAPE, w + "need 0 <= T <= 2^28, 0 <= n_seqs <= 2^22");
     if (d->n_heads < 1 || d->n_heads > 65535 || d->n_kv < 1 || d->n_heads % d->n_kv)
         return set_error(ctx, REALQ_ERR_SHAPE, w + "need 1 <= n_heads <= 65535, n_kv >= 1 dividing n_heads");
+    if ((d->T / 128 + d->n_seqs) * d->n_heads > (int64_t)1 << 23)
+        return set_error(ctx, REALQ_ERR_SHAPE, w + "need (T / 128 + n_seqs) n_heads <= 2^23");
     if (d->head_dim < 8 || d->head_dim > 256 || d->head_dim % 8)
         return set_error(ctx, REALQ_ERR_SHAPE, w + "head_dim must be a multiple of 8, 8 .. 256");
     if (!(d->scale >= 0.f) || std::isinf(d->scale))
@@ -85,8 +87,8 @@ int check_attention(realq_ctx* ctx, const realq_attention_desc* d, const char* w
 int check_heads(realq_ctx* ctx, const char* who, const char* name, const void* p, int64_t ld, int64_t heads, int hd) {
     const std::string w = std::string(who) + ": " + name;
     if (!p) return set_error(ctx, REALQ_ERR_INVALID_ARG, w + " is NULL");
-    if (ld < heads * hd || ld % 8 || ld > kMostRows)
-        return set_error(ctx, REALQ_ERR_SHAPE, w + ": row stride must be a multiple of 8 and hold all heads");
+    if (ld < heads * hd || ld % 8 || ld > ((int64_t)1 << 24))
+        return set_error(ctx, REALQ_ERR_SHAPE, w + ": row stride must be a multiple of 8, hold all heads and be at most 2^24");
     if (!aligned(p, 16)) return set_error(ctx, REALQ_ERR_INVALID_ARG, w + " must be aligned to 16 bytes");
     return REALQ_OK;
 }

@@ -133,8 +133,10 @@ def attention(L):
                      (dict(dQ=None), -1), (dict(dK=None), -1), (dict(dV=None), -1), (dict(lddq=508), -2),
                      (dict(lddk=120), -2), (dict(dV=at(buf(11), 2)), -1)):
         refused(L, code, "packed_attention_backward", g, *bwd(desc(), **kw))
+    refused(L, -2, "2^23", f, *fwd(desc(T=1 << 28, n_seqs=1 << 10)))
+    refused(L, -2, "2^24", f, *fwd(desc(ldq=(1 << 24) + 8)))
     for hd in (8, 64, 128, 256):
-        big = desc(T=1 << 28, n_seqs=1 << 22, head_dim=hd, ldq=8 * hd, ldk=2 * hd, ldv=2 * hd)
+        big = desc(T=(1 << 27) - 128, n_seqs=1, head_dim=hd, ldq=8 * hd, ldk=2 * hd, ldv=2 * hd)
         assert launched(L, f, *fwd(big, ldo=8 * hd)) >= 1
         assert launched(L, g, *bwd(big, ldo=8 * hd, lddo=8 * hd, lddq=8 * hd, lddk=2 * hd, lddv=2 * hd)) >= 1
 
