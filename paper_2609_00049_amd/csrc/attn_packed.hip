@@ -185,19 +185,6 @@ __device__ __forceinline__ void clear_rest(uint16_t* lds, int hd) {
     __syncthreads();
 }
 
-// rows r0 .. r0 + ROWS - 1 (past the last one: the last one again) of one head into an LDS tile
-template <int HD, int ROWS, int NT>
-__device__ __forceinline__ void stage(const uint16_t* __restrict__ g, int64_t ld, int hd, int r0, int len,
-                                      uint16_t* lds) {
-    constexpr int CH = HD / 8;
-#pragma unroll
-    for (int c = 0; c < ROWS * CH / NT; ++c) {
-        const int i = threadIdx.x + c * NT, r = i / CH, ch = i % CH;
-        u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (ch * 8 < hd) v = *reinterpret_cast<const u16x8*>(g + (int64_t)min(r0 + r, len - 1) * ld + ch * 8);
-        *reinterpret_cast<u16x8*>(lds + place<HD>(r, ch)) = v;
-    }
-}
 // row `row` of one head as an operand held in registers
 template <int HD>
 __device__ __forceinline__ void hold(const uint16_t* __restrict__ g, int hd, int lane, bf16x8 (&f)[HD / 16]) {
@@ -332,23 +319,32 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
     if (lse && lane < 32) lse[(int64_t)h * a.T + row] = m * a.scale + kLn2 * __builtin_amdgcn_logf(l);
 }
 
-// dQ (and delta) of 128 queries: loops over the key tiles they see.
+// dQ (and delta) of 128 queries, 32 a wave, over the key tiles they see, in two LDS buffers.  As in the
+// forward a query's scores are one lane's: S^T = K Q^T, dP^T = V dO^T, and dS^T goes into dQ^T += K^T dS^T.
 template <int HD>
-__global__ __launch_bounds__(NT) void attn_dq_kernel(AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo,
-                                                     const float* __restrict__ lse, const uint16_t* __restrict__ dO,
-                                                     int64_t lddo, float* __restrict__ delta,
-                                                     uint16_t* __restrict__ dQ, int64_t lddq) {
-    constexpr int BN = 32;
-    __shared__ __attribute__((aligned(16))) uint16_t sk[BN * HD], sv[BN * HD];
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+__global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
+    AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
+    const uint16_t* __restrict__ dO, int64_t lddo, float* __restrict__ delta, uint16_t* __restrict__ dQ, int64_t lddq,
+    int64_t tiles) {
+    constexpr int BN = HD <= 128 ? 64 : 32;
+    __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
+    int64_t slot;
+    int h;
+    item_of(tiles, slot, h);
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
     if (!sq.any) return;
-    const int h = blockIdx.y, kv = h / (a.n_heads / a.n_kv);
+    const int kv = h / (a.n_heads / a.n_kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int q0 = sq.tile * BM + wave * 32;
     const int qi = min(q0 + (lane & 31), sq.len - 1);
     const int64_t row = sq.begin + qi;
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
+    clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
+    const Loader<HD, BN, NT / 64> loader(a.hd);
+    const int keys = min((sq.tile + 1) * BM, sq.len);
+    loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
+    loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
     bf16x8 qf[HD / 16], df[HD / 16];
     hold<HD>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
     hold<HD>(dO + row * lddo + h * a.hd, a.hd, lane, df);
@@ -368,29 +364,38 @@ __global__ __launch_bounds__(NT) void attn_dq_kernel(AttnArgs a, const uint16_t*
     f32x16 g[HD / 32];
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) g[t] = zero16();
-    const int keys = min((sq.tile + 1) * BM, sq.len);
-    for (int k0 = 0; k0 < keys; k0 += BN) {
-        __syncthreads();
-        stage<HD, BN, NT>(K, a.ldk, a.hd, k0, sq.len, sk);
-        stage<HD, BN, NT>(V, a.ldv, a.hd, k0, sq.len, sv);
-        __syncthreads();
-        if (k0 > q0 + 31) continue;
-        f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-        for (int u = 0; u < HD / 16; ++u) {
-            s = mfma(row_frag<HD>(sk, 0, u, lane), qf[u], s);
-            dp = mfma(row_frag<HD>(sv, 0, u, lane), df[u], dp);
+    int buf = 0;
+    for (int k0 = 0; k0 < keys; k0 += BN, buf ^= 1) {
+        vm_wait<0>();
+        block_sync();
+        if (k0 + BN < keys) {
+            loader.load(K, a.ldk, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][0]));
+            loader.load(V, a.ldv, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][1]));
         }
+        const uint16_t* sk = kv_lds[buf][0];
+        const uint16_t* sv = kv_lds[buf][1];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float p = __builtin_amdgcn_exp2f(s[e] * c - L);
-            s[e] = k0 + crow(e, lane) > qi ? 0.f : p * (dp[e] - dl);
-        }
+        for (int b = 0; b < BN / 32; ++b) {
+            const int kb = k0 + 32 * b;
+            if (kb > q0 + 31) continue;
+            f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            const bf16x8 d = pack_frag(s, x);
+            for (int u = 0; u < HD / 16; ++u) {
+                s = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s);
+                dp = mfma(row_frag<HD>(sv, 32 * b, u, lane), df[u], dp);
+            }
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 16 * x, t, lane), d, g[t]);
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
+            if (kb + 31 > q0)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (kb + crow(e, lane) > qi) s[e] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const bf16x8 d = pack_frag(s, x);
+#pragma unroll
+                for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
+            }
         }
     }
     if (!live) return;
@@ -407,22 +412,29 @@ __global__ __launch_bounds__(NT) void attn_dq_kernel(AttnArgs a, const uint16_t*
         }
 }
 
-// dK and dV of 128 keys: loops over the query heads of their key/value head and the queries that see them,
-// in that order, so the sums have one order.
+// dK and dV of 128 keys, 32 a wave: the query heads of their key/value head, and of each the queries that see
+// them, in that order, so the sums have one order.  Here a key is one lane's: S = Q K^T and dP = dO V^T, and
+// P^T and dS^T are the first operands of dV += P^T dO and dK += dS^T Q.
 template <int HD>
-__global__ __launch_bounds__(NT) void attn_dkv_kernel(AttnArgs a, const float* __restrict__ lse,
-                                                      const uint16_t* __restrict__ dO, int64_t lddo,
-                                                      const float* __restrict__ delta, uint16_t* __restrict__ dK,
-                                                      int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv) {
-    constexpr int BQ = 32;
-    __shared__ __attribute__((aligned(16))) uint16_t sqr[BQ * HD], sdo[BQ * HD];
-    __shared__ __attribute__((aligned(16))) float sl[BQ], sd[BQ];
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, blockIdx.x);
+__global__ __launch_bounds__(NT, HD <= 64 ? 2 : 1) void attn_dkv_kernel(
+    AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
+    const float* __restrict__ delta, uint16_t* __restrict__ dK, int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv,
+    int64_t tiles) {
+    constexpr int BQ = HD <= 128 ? 64 : 32;
+    __shared__ __attribute__((aligned(16))) uint16_t qd_lds[2][2][BQ * HD];
+    __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];  // lse in units of log 2, delta
+    int64_t slot;
+    int kv;
+    item_of(tiles, slot, kv);
+    slot = tiles - 1 - slot;  // the first keys of a sequence are seen by the most queries
+    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
     if (!sq.any) return;
-    const int kv = blockIdx.y, group = a.n_heads / a.n_kv;
+    const int group = a.n_heads / a.n_kv;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int k0 = sq.tile * BM + wave * 32;
     const int ki = min(k0 + (lane & 31), sq.len - 1);
+    clear_rest<HD, 4 * BQ, NT>(qd_lds[0][0], a.hd);
+    const Loader<HD, BQ, NT / 64> loader(a.hd);
     bf16x8 kf[HD / 16], vf[HD / 16];
     hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
     hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
@@ -430,45 +442,74 @@ __global__ __launch_bounds__(NT) void attn_dkv_kernel(AttnArgs a, const float* _
     f32x16 gk[HD / 32], gv[HD / 32];
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) gk[t] = gv[t] = zero16();
-    for (int h = kv * group; h < (kv + 1) * group; ++h) {
-        const uint16_t* Q = a.q + sq.begin * a.ldq + h * a.hd;
-        const uint16_t* D = dO + sq.begin * lddo + h * a.hd;
-        const float* Lr = lse + (int64_t)h * a.T + sq.begin;
-        const float* Dr = delta + (int64_t)h * a.T + sq.begin;
-        for (int q0 = sq.tile * BM; q0 < sq.len; q0 += BQ) {
-            __syncthreads();
-            stage<HD, BQ, NT>(Q, a.ldq, a.hd, q0, sq.len, sqr);
-            stage<HD, BQ, NT>(D, lddo, a.hd, q0, sq.len, sdo);
-            if (threadIdx.x < BQ) {
-                const int r = min(q0 + (int)threadIdx.x, sq.len - 1);
-                sl[threadIdx.x] = Lr[r] * kLog2e;
-                sd[threadIdx.x] = Dr[r];
-            }
-            __syncthreads();
-            if (q0 + BQ - 1 < k0) continue;
+    const int first = sq.tile * BM, steps = (sq.len - first + BQ - 1) / BQ, total = steps * group;
+    int lh = kv * group, lq = first;  // head and query tile of the next load
+    float pl = 0.f, pd = 0.f;         // its statistics on their way to LDS
+    auto fetch = [&](int buf) {
+        loader.load(a.q + sq.begin * a.ldq + (int64_t)lh * a.hd, a.ldq, lq, sq.len, lds_at(qd_lds[buf][0]));
+        loader.load(dO + sq.begin * lddo + (int64_t)lh * a.hd, lddo, lq, sq.len, lds_at(qd_lds[buf][1]));
+        if (threadIdx.x < BQ) {
+            const int64_t r = (int64_t)lh * a.T + sq.begin + min(lq + (int)threadIdx.x, sq.len - 1);
+            pl = lse[r] * kLog2e;
+            pd = delta[r];
+        }
+        lq += BQ;
+        if (lq >= sq.len) {
+            lq = first;
+            ++lh;
+        }
+    };
+    auto keep = [&](int buf) {
+        if (threadIdx.x < BQ) {
+            stat[buf][0][threadIdx.x] = pl;
+            stat[buf][1][threadIdx.x] = pd;
+        }
+    };
+    fetch(0);
+    keep(0);
+    int q0 = first, buf = 0;
+    for (int i = 0; i < total; ++i, buf ^= 1) {
+        vm_wait<0>();
+        __syncthreads();
+        const bool more = i + 1 < total;
+        if (more) fetch(buf ^ 1);
+        const uint16_t* sqr = qd_lds[buf][0];
+        const uint16_t* sdo = qd_lds[buf][1];
+#pragma unroll
+        for (int b = 0; b < BQ / 32; ++b) {
+            const int qb = q0 + 32 * b;
+            if (qb + 31 < k0) continue;
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int u = 0; u < HD / 16; ++u) {
-                s = mfma(row_frag<HD>(sqr, 0, u, lane), kf[u], s);
-                dp = mfma(row_frag<HD>(sdo, 0, u, lane), vf[u], dp);
+                s = mfma(row_frag<HD>(sqr, 32 * b, u, lane), kf[u], s);
+                dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), vf[u], dp);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int r = crow(e, lane), qi = q0 + r;
-                const float p = qi < ki || qi >= sq.len ? 0.f : __builtin_amdgcn_exp2f(s[e] * c - sl[r]);
-                s[e] = p;
-                dp[e] = p * (dp[e] - sd[r]);
+                const int r = 32 * b + crow(e, lane);
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -stat[buf][0][r]));
+                dp[e] = s[e] * (dp[e] - stat[buf][1][r]);
             }
+            if (qb < k0 + 31 || qb + 32 > sq.len)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int qi = qb + crow(e, lane);
+                    if (qi < ki || qi >= sq.len) s[e] = dp[e] = 0.f;
+                }
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const bf16x8 p = pack_frag(s, x), d = pack_frag(dp, x);
 #pragma unroll
                 for (int t = 0; t < HD / 32; ++t) {
-                    gv[t] = mfma(p, col_frag<HD>(sdo, 16 * x, t, lane), gv[t]);
-                    gk[t] = mfma(d, col_frag<HD>(sqr, 16 * x, t, lane), gk[t]);
+                    gv[t] = mfma(p, col_frag<HD>(sdo, 32 * b + 16 * x, t, lane), gv[t]);
+                    gk[t] = mfma(d, col_frag<HD>(sqr, 32 * b + 16 * x, t, lane), gk[t]);
                 }
             }
         }
+        if (more) keep(buf ^ 1);
+        q0 += BQ;
+        if (q0 >= sq.len) q0 = first;
     }
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t)
@@ -499,11 +540,11 @@ hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, floa
 hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ldo, const float* lse,
                                 const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ, int64_t lddq,
                                 uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st) {
-    const dim3 gq((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_heads);
-    const dim3 gk((unsigned)(a.T / BM + a.n_seqs), (unsigned)a.n_kv);
-    RQ_HEAD_DIM(attn_dq_kernel, gq, a, O, ldo, lse, dO, lddo, delta, dQ, lddq);
+    const int64_t tiles = a.T / BM + a.n_seqs;
+    const dim3 gq((unsigned)(tiles * a.n_heads)), gk((unsigned)(tiles * a.n_kv));
+    RQ_HEAD_DIM(attn_dq_kernel, gq, a, O, ldo, lse, dO, lddo, delta, dQ, lddq, tiles);
     if (const hipError_t e = hipGetLastError()) return e;
-    RQ_HEAD_DIM(attn_dkv_kernel, gk, a, lse, dO, lddo, delta, dK, lddk, dV, lddv);
+    RQ_HEAD_DIM(attn_dkv_kernel, gk, a, lse, dO, lddo, delta, dK, lddk, dV, lddv, tiles);
     return hipGetLastError();
 }
 
