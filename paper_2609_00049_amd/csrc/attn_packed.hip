@@ -148,9 +148,9 @@ struct Loader {
     int row, wave;
     uint32_t chunk[D];  // byte offset of this lane's chunk in its row
     bool on[D];
-    __device__ Loader(int hd) {
+    __device__ Loader(int hd, int wave_) {
         const int lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wave = __builtin_amdgcn_readfirstlane(wave_);
         row = wave * RPI + lane / CH;
 #pragma unroll
         for (int d = 0; d < D; ++d) {
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
     clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
-    const Loader<HD, BN, NT / 64> loader(a.hd);
+    const Loader<HD, BN, NT / 64> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
     loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
     loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
     clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
-    const Loader<HD, BN, NT / 64> loader(a.hd);
+    const Loader<HD, BN, NT / 64> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
     loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
     loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
@@ -412,17 +412,22 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
         }
 }
 
-// dK and dV of 128 keys, 32 a wave: the query heads of their key/value head, and of each the queries that see
-// them, in that order, so the sums have one order.  Here a key is one lane's: S = Q K^T and dP = dO V^T, and
-// P^T and dS^T are the first operands of dV += P^T dO and dK += dS^T Q.
-template <int HD>
-__global__ __launch_bounds__(NT, HD <= 64 ? 2 : 1) void attn_dkv_kernel(
+// dK and dV of 128 keys, 32 a wave: the query heads of their key/value head, and of each the tiles of queries
+// that see them.  Here a key is one lane's: S = Q K^T and dP = dO V^T, and P^T and dS^T are the first operands
+// of dV += P^T dO and dK += dS^T Q.  GROUPS groups of 4 waves take the tiles in turn, each from LDS buffers of
+// its own, and their sums are added at the end in one order: a block of 8 waves puts two on a SIMD, one
+// multiplying while the other forms P and dS, without making the longest block (the first keys of a long
+// sequence, which sets the time) any longer.  KL: K is read from LDS, which leaves 8 waves of 128 channels
+// their 256 registers; DK, DV: what this launch forms (both, or one each where both do not fit).
+template <int HD, int GROUPS, bool KL, bool DK, bool DV>
+__global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
     const float* __restrict__ delta, uint16_t* __restrict__ dK, int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv,
     int64_t tiles) {
-    constexpr int BQ = HD <= 128 ? 64 : 32;
-    __shared__ __attribute__((aligned(16))) uint16_t qd_lds[2][2][BQ * HD];
-    __shared__ __attribute__((aligned(16))) float stat[2][2][BQ];  // lse in units of log 2, delta
+    constexpr int BQ = HD <= 64 ? 64 : 32, THREADS = 256 * GROUPS, ACC = HD / 32;
+    __shared__ __attribute__((aligned(16))) uint16_t qd_lds[GROUPS][2][2][BQ * HD];
+    __shared__ __attribute__((aligned(16))) uint16_t k_lds[KL ? BM * HD : 8];
+    __shared__ __attribute__((aligned(16))) float stat[GROUPS][2][2][BQ];  // lse in units of log 2, delta
     int64_t slot;
     int kv;
     item_of(tiles, slot, kv);
@@ -430,51 +435,59 @@ __global__ __launch_bounds__(NT, HD <= 64 ? 2 : 1) void attn_dkv_kernel(
     const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
     if (!sq.any) return;
     const int group = a.n_heads / a.n_kv;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, tid = threadIdx.x & 255;
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = all >> 2, wave = all & 3;
     const int k0 = sq.tile * BM + wave * 32;
     const int ki = min(k0 + (lane & 31), sq.len - 1);
-    clear_rest<HD, 4 * BQ, NT>(qd_lds[0][0], a.hd);
-    const Loader<HD, BQ, NT / 64> loader(a.hd);
-    bf16x8 kf[HD / 16], vf[HD / 16];
-    hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
-    hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
+    clear_rest<HD, GROUPS * 4 * BQ, THREADS>(qd_lds[0][0][0], a.hd);
+    if constexpr (KL) {
+        clear_rest<HD, BM, THREADS>(k_lds, a.hd);
+        Loader<HD, BM, 4 * GROUPS>(a.hd, threadIdx.x >> 6)
+            .load(a.k + sq.begin * a.ldk + kv * a.hd, a.ldk, sq.tile * BM, sq.len, lds_at(k_lds));
+    }
+    const Loader<HD, BQ, 4> loader(a.hd, wave);
+    bf16x8 kf[KL ? 1 : HD / 16], vf[DK ? HD / 16 : 1];
+    if constexpr (!KL) hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
+    if constexpr (DK) hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
     const float c = a.scale * kLog2e;
-    f32x16 gk[HD / 32], gv[HD / 32];
+    f32x16 gk[DK ? ACC : 1], gv[DV ? ACC : 1];
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t) gk[t] = gv[t] = zero16();
+    for (int t = 0; t < ACC; ++t) {
+        if constexpr (DK) gk[t] = zero16();
+        if constexpr (DV) gv[t] = zero16();
+    }
     const int first = sq.tile * BM, steps = (sq.len - first + BQ - 1) / BQ, total = steps * group;
-    int lh = kv * group, lq = first;  // head and query tile of the next load
-    float pl = 0.f, pd = 0.f;         // its statistics on their way to LDS
-    auto fetch = [&](int buf) {
-        loader.load(a.q + sq.begin * a.ldq + (int64_t)lh * a.hd, a.ldq, lq, sq.len, lds_at(qd_lds[buf][0]));
-        loader.load(dO + sq.begin * lddo + (int64_t)lh * a.hd, lddo, lq, sq.len, lds_at(qd_lds[buf][1]));
-        if (threadIdx.x < BQ) {
-            const int64_t r = (int64_t)lh * a.T + sq.begin + min(lq + (int)threadIdx.x, sq.len - 1);
+    auto fetch = [&](int i, int buf, float& pl, float& pd) {  // tile i: its head and queries
+        const int h = kv * group + i / steps, q = first + i % steps * BQ;
+        loader.load(a.q + sq.begin * a.ldq + (int64_t)h * a.hd, a.ldq, q, sq.len, lds_at(qd_lds[grp][buf][0]));
+        loader.load(dO + sq.begin * lddo + (int64_t)h * a.hd, lddo, q, sq.len, lds_at(qd_lds[grp][buf][1]));
+        if (tid < BQ) {
+            const int64_t r = (int64_t)h * a.T + sq.begin + min(q + tid, sq.len - 1);
             pl = lse[r] * kLog2e;
-            pd = delta[r];
-        }
-        lq += BQ;
-        if (lq >= sq.len) {
-            lq = first;
-            ++lh;
+            if constexpr (DK) pd = delta[r];
         }
     };
+    float pl = 0.f, pd = 0.f;  // the next tile's statistics on their way to LDS
     auto keep = [&](int buf) {
-        if (threadIdx.x < BQ) {
-            stat[buf][0][threadIdx.x] = pl;
-            stat[buf][1][threadIdx.x] = pd;
+        if (tid < BQ) {
+            stat[grp][buf][0][tid] = pl;
+            if constexpr (DK) stat[grp][buf][1][tid] = pd;
         }
     };
-    fetch(0);
-    keep(0);
-    int q0 = first, buf = 0;
-    for (int i = 0; i < total; ++i, buf ^= 1) {
+    if (grp < total) {
+        fetch(grp, 0, pl, pd);
+        keep(0);
+    }
+    int buf = 0;
+    for (int i = grp; i - grp < total; i += GROUPS, buf ^= 1) {
         vm_wait<0>();
         __syncthreads();
-        const bool more = i + 1 < total;
-        if (more) fetch(buf ^ 1);
-        const uint16_t* sqr = qd_lds[buf][0];
-        const uint16_t* sdo = qd_lds[buf][1];
+        if (i >= total) break;  // the last round of the later groups; all waves have passed the same barriers
+        const bool more = i + GROUPS < total;
+        if (more) fetch(i + GROUPS, buf ^ 1, pl, pd);
+        const int q0 = first + i % steps * BQ;
+        const uint16_t* sqr = qd_lds[grp][buf][0];
+        const uint16_t* sdo = qd_lds[grp][buf][1];
 #pragma unroll
         for (int b = 0; b < BQ / 32; ++b) {
             const int qb = q0 + 32 * b;
@@ -482,14 +495,17 @@ __global__ __launch_bounds__(NT, HD <= 64 ? 2 : 1) void attn_dkv_kernel(
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int u = 0; u < HD / 16; ++u) {
-                s = mfma(row_frag<HD>(sqr, 32 * b, u, lane), kf[u], s);
-                dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), vf[u], dp);
+                bf16x8 k;
+                if constexpr (KL) k = row_frag<HD>(k_lds, wave * 32, u, lane);
+                else k = kf[u];
+                s = mfma(row_frag<HD>(sqr, 32 * b, u, lane), k, s);
+                if constexpr (DK) dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), vf[u], dp);
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int r = 32 * b + crow(e, lane);
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -stat[buf][0][r]));
-                dp[e] = s[e] * (dp[e] - stat[buf][1][r]);
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -stat[grp][buf][0][r]));
+                if constexpr (DK) dp[e] = s[e] * (dp[e] - stat[grp][buf][1][r]);
             }
             if (qb < k0 + 31 || qb + 32 > sq.len)
 #pragma unroll
@@ -501,25 +517,43 @@ __global__ __launch_bounds__(NT, HD <= 64 ? 2 : 1) void attn_dkv_kernel(
             for (int x = 0; x < 2; ++x) {
                 const bf16x8 p = pack_frag(s, x), d = pack_frag(dp, x);
 #pragma unroll
-                for (int t = 0; t < HD / 32; ++t) {
-                    gv[t] = mfma(p, col_frag<HD>(sdo, 32 * b + 16 * x, t, lane), gv[t]);
-                    gk[t] = mfma(d, col_frag<HD>(sqr, 32 * b + 16 * x, t, lane), gk[t]);
+                for (int t = 0; t < ACC; ++t) {
+                    if constexpr (DV) gv[t] = mfma(p, col_frag<HD>(sdo, 32 * b + 16 * x, t, lane), gv[t]);
+                    if constexpr (DK) gk[t] = mfma(d, col_frag<HD>(sqr, 32 * b + 16 * x, t, lane), gk[t]);
                 }
             }
         }
         if (more) keep(buf ^ 1);
-        q0 += BQ;
-        if (q0 >= sq.len) q0 = first;
+    }
+    if constexpr (GROUPS == 2) {  // the second group's sums through the LDS of the tiles, 32 channels at a time
+        float* const sum = reinterpret_cast<float*>(qd_lds[0][0][0]) + tid;
+        static_assert(sizeof(qd_lds) >= 16 * 256 * 4 && DK && DV, "16 sums a thread");
+        auto join = [&](f32x16& v) {
+            __syncthreads();
+            if (grp == 1)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[e * 256] = v[e];
+            __syncthreads();
+            if (grp == 0)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] += sum[e * 256];
+        };
+#pragma unroll
+        for (int t = 0; t < ACC; ++t) {
+            join(gk[t]);
+            join(gv[t]);
+        }
+        if (grp == 1) return;
     }
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t)
+    for (int t = 0; t < ACC; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int r = k0 + crow(e, lane), ch = 32 * t + (lane & 31);
             if (r >= sq.len || ch >= a.hd) continue;
             const int64_t at = sq.begin + r;
-            dK[at * lddk + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)(gk[t][e] * a.scale));
-            dV[at * lddv + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)gv[t][e]);
+            if constexpr (DK) dK[at * lddk + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)(gk[t][e] * a.scale));
+            if constexpr (DV) dV[at * lddv + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)gv[t][e]);
         }
 }
 
@@ -544,7 +578,18 @@ hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ld
     const dim3 gq((unsigned)(tiles * a.n_heads)), gk((unsigned)(tiles * a.n_kv));
     RQ_HEAD_DIM(attn_dq_kernel, gq, a, O, ldo, lse, dO, lddo, delta, dQ, lddq, tiles);
     if (const hipError_t e = hipGetLastError()) return e;
-    RQ_HEAD_DIM(attn_dkv_kernel, gk, a, lse, dO, lddo, delta, dK, lddk, dV, lddv, tiles);
+#define RQ_DKV(HD, GROUPS, KL, DK, DV)                                                                             \
+    hipLaunchKernelGGL((attn_dkv_kernel<HD, GROUPS, KL, DK, DV>), gk, dim3(256 * GROUPS), 0, st, a, lse, dO, lddo, \
+                       delta, dK, lddk, dV, lddv, tiles)
+    if (a.hd <= 64) {
+        RQ_DKV(64, 2, false, true, true);
+    } else if (a.hd <= 128) {
+        RQ_DKV(128, 2, true, true, true);
+    } else {
+        RQ_DKV(256, 1, false, false, true);
+        RQ_DKV(256, 1, false, true, false);
+    }
+#undef RQ_DKV
     return hipGetLastError();
 }
 
