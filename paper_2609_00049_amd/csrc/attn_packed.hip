@@ -89,6 +89,22 @@ __device__ __forceinline__ f32x16 zero16() {
 // Row of register e of a result, in this lane.
 __device__ __forceinline__ int crow(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
 
+// Order of a phase of `reads` LDS reads that feed `products` matrix instructions: `ahead` reads first, so that
+// none is waited for right after it is issued (left alone, the compiler reads two and waits).
+constexpr int AHEAD = 6;
+template <int READS, int PRODUCTS, int FIRST, int I = 0>
+__device__ __forceinline__ void order_reads() {
+    if constexpr (I == 0) __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+    if constexpr (I < READS - FIRST) {
+        constexpr int DUE = PRODUCTS * (I + 1) / READS - PRODUCTS * I / READS;
+        if constexpr (DUE > 0) __builtin_amdgcn_sched_group_barrier(0x008, DUE, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        order_reads<READS, PRODUCTS, FIRST, I + 1>();
+    } else {
+        __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS - PRODUCTS * I / READS, 0);
+    }
+}
+
 struct Seq {
     int64_t begin;  // first row
     int len;        // rows
@@ -262,6 +278,7 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
         for (int u = 0; u < HD / 16; ++u)
 #pragma unroll
             for (int b = 0; b < NB; ++b) s[b] = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s[b]);
+        order_reads<HD / 16 * NB, HD / 16 * NB, AHEAD>();
         if (k0 + BN - 1 > q0)  // a tile that some query of the wave sees in part
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -384,12 +401,13 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
                 s = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s);
                 dp = mfma(row_frag<HD>(sv, 32 * b, u, lane), df[u], dp);
             }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
+            order_reads<HD / 8, HD / 8, AHEAD>();
             if (kb + 31 > q0)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (kb + crow(e, lane) > qi) s[e] = 0.f;
+                    if (kb + crow(e, lane) > qi) s[e] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const bf16x8 d = pack_frag(s, x);
@@ -424,9 +442,9 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
     const float* __restrict__ delta, uint16_t* __restrict__ dK, int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv,
     int64_t tiles) {
-    constexpr int BQ = HD <= 64 ? 64 : 32, THREADS = 256 * GROUPS, ACC = HD / 32;
+    constexpr int BQ = 32, THREADS = 256 * GROUPS, ACC = HD / 32;
     __shared__ __attribute__((aligned(16))) uint16_t qd_lds[GROUPS][2][2][BQ * HD];
-    __shared__ __attribute__((aligned(16))) uint16_t k_lds[KL ? BM * HD : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][KL ? BM * HD : 8];
     __shared__ __attribute__((aligned(16))) float stat[GROUPS][2][2][BQ];  // lse in units of log 2, delta
     int64_t slot;
     int kv;
@@ -441,14 +459,15 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     const int ki = min(k0 + (lane & 31), sq.len - 1);
     clear_rest<HD, GROUPS * 4 * BQ, THREADS>(qd_lds[0][0][0], a.hd);
     if constexpr (KL) {
-        clear_rest<HD, BM, THREADS>(k_lds, a.hd);
-        Loader<HD, BM, 4 * GROUPS>(a.hd, threadIdx.x >> 6)
-            .load(a.k + sq.begin * a.ldk + kv * a.hd, a.ldk, sq.tile * BM, sq.len, lds_at(k_lds));
+        clear_rest<HD, 2 * BM, THREADS>(kv_lds[0], a.hd);
+        const Loader<HD, BM, 4 * GROUPS> keys(a.hd, all);
+        keys.load(a.k + sq.begin * a.ldk + kv * a.hd, a.ldk, sq.tile * BM, sq.len, lds_at(kv_lds[0]));
+        keys.load(a.v + sq.begin * a.ldv + kv * a.hd, a.ldv, sq.tile * BM, sq.len, lds_at(kv_lds[1]));
     }
     const Loader<HD, BQ, 4> loader(a.hd, wave);
-    bf16x8 kf[KL ? 1 : HD / 16], vf[DK ? HD / 16 : 1];
+    bf16x8 kf[KL ? 1 : HD / 16], vf[DK && !KL ? HD / 16 : 1];
     if constexpr (!KL) hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
-    if constexpr (DK) hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
+    if constexpr (DK && !KL) hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
     const float c = a.scale * kLog2e;
     f32x16 gk[DK ? ACC : 1], gv[DV ? ACC : 1];
 #pragma unroll
@@ -495,33 +514,46 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
             for (int u = 0; u < HD / 16; ++u) {
-                bf16x8 k;
-                if constexpr (KL) k = row_frag<HD>(k_lds, wave * 32, u, lane);
-                else k = kf[u];
+                bf16x8 k, v;
+                if constexpr (KL) {
+                    k = row_frag<HD>(kv_lds[0], wave * 32, u, lane);
+                    v = row_frag<HD>(kv_lds[1], wave * 32, u, lane);
+                } else {
+                    k = kf[u];
+                    v = vf[DK ? u : 0];
+                }
                 s = mfma(row_frag<HD>(sqr, 32 * b, u, lane), k, s);
-                if constexpr (DK) dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), vf[u], dp);
+                if constexpr (DK) dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), v, dp);
             }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int r = 32 * b + crow(e, lane);
-                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -stat[grp][buf][0][r]));
-                if constexpr (DK) dp[e] = s[e] * (dp[e] - stat[grp][buf][1][r]);
-            }
+            order_reads<HD / 16 * (1 + KL) * (1 + DK), HD / 16 * (1 + DK), KL ? 8 : 6>();
             if (qb < k0 + 31 || qb + 32 > sq.len)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int qi = qb + crow(e, lane);
-                    if (qi < ki || qi >= sq.len) s[e] = dp[e] = 0.f;
+                    if (qi < ki || qi >= sq.len) s[e] = -INFINITY;
                 }
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 p = pack_frag(s, x), d = pack_frag(dp, x);
+            for (int q = 0; q < 4; ++q) {
+                const int r = 32 * b + 8 * q + 4 * (lane >> 5);
+                const f32x4 L = *reinterpret_cast<const f32x4*>(&stat[grp][buf][0][r]);
+                const f32x4 d = *reinterpret_cast<const f32x4*>(&stat[grp][buf][1][r]);
 #pragma unroll
-                for (int t = 0; t < ACC; ++t) {
-                    if constexpr (DV) gv[t] = mfma(p, col_frag<HD>(sdo, 32 * b + 16 * x, t, lane), gv[t]);
-                    if constexpr (DK) gk[t] = mfma(d, col_frag<HD>(sqr, 32 * b + 16 * x, t, lane), gk[t]);
+                for (int x = 0; x < 4; ++x) {
+                    s[4 * q + x] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + x], c, -L[x]));
+                    if constexpr (DK) dp[4 * q + x] = s[4 * q + x] * (dp[4 * q + x] - d[x]);
                 }
             }
+            const bf16x8 p[2] = {pack_frag(s, 0), pack_frag(s, 1)}, d[2] = {pack_frag(dp, 0), pack_frag(dp, 1)};
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int t = 0; t < ACC; ++t) {
+                    if constexpr (DV) gv[t] = mfma(p[x], col_frag<HD>(sdo, 32 * b + 16 * x, t, lane), gv[t]);
+                    if constexpr (DK) gk[t] = mfma(d[x], col_frag<HD>(sqr, 32 * b + 16 * x, t, lane), gk[t]);
+                }
+            order_reads<4 * ACC * (DK + DV), 2 * ACC * (DK + DV), 8>();
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (more) keep(buf ^ 1);
     }
