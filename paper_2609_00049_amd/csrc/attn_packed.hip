@@ -217,13 +217,58 @@ constexpr int NT = 256, BM = 128;
 
 }  // namespace
 
-// This block's item: each XCD (blocks are dealt to the 8 round-robin) takes a run of consecutive heads, whose
-// keys and values its L2 then holds; within a head the last tiles, which see the most keys, come first.
-__device__ __forceinline__ void item_of(int64_t tiles, int64_t& slot, int& head) {
-    const int64_t n = gridDim.x, q = n >> 3, r = n & 7, x = blockIdx.x & 7;
-    const int64_t L = x * q + min(x, r) + (blockIdx.x >> 3);
-    head = (int)(L / tiles);
-    slot = tiles - 1 - L % tiles;
+// The block's head and its rank among the head's tiles, most work first.  Blocks are dealt to the 8 XCDs
+// round-robin: where the heads divide among them, an XCD takes consecutive ones (whose keys and values its L2
+// then holds), the same tile of all of them before the next tile.
+__device__ __forceinline__ void item_of(int heads, int64_t& rank, int& head) {
+    const uint32_t b = blockIdx.x;
+    if (heads % 8 == 0) {
+        const uint32_t per = heads / 8, i = b >> 3;
+        head = (int)((b & 7) * per + i % per);
+        rank = i / per;
+    } else {
+        head = (int)(b % heads);
+        rank = b / heads;
+    }
+}
+
+// The rank-th tile of all sequences, by its number of tiles before it (REVERSE: behind it), the largest first:
+// long blocks start early and the last ones are short (4 sequences of 2048 tokens, forward: 187 us by the rows'
+// order, 162 us so).  Up to 64 sequences lane b counts the tiles of sequence b, and 64 values of x at once are
+// tried for the number of tiles with x or more before them; past 64 the rows' order serves, as blocks are many.
+template <int BM, bool REVERSE>
+__device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64_t n_seqs, int64_t T, int64_t tiles,
+                                           int64_t rank) {
+    if (n_seqs > 64) return find_tile<BM>(cu, n_seqs, T, REVERSE ? rank : tiles - 1 - rank);
+    const int lane = threadIdx.x & 63, n = (int)n_seqs;
+    const int from = (int)min(max((int64_t)cu[min(lane, n)], (int64_t)0), T);
+    const int to = (int)min(max((int64_t)cu[min(lane + 1, n)], (int64_t)0), T);
+    const int len = max(to - from, 0), mine = lane < n ? (len + BM - 1) / BM : 0;
+    auto count = [&](int x) {  // tiles with x or more before them
+        int c = 0;
+        for (int b = 0; b < n; ++b) c += max(__builtin_amdgcn_readlane(mine, b) - x, 0);
+        return c;
+    };
+    int lo = 0, span = (int)(T / BM) + 1;
+    uint64_t v;
+    do {
+        const int step = (span + 63) / 64;
+        v = __ballot(count(lo + lane * step) > (int)rank);
+        const int k = v ? __builtin_popcountll(v) - 1 : 0;
+        lo += k * step;
+        span = step;
+    } while (span > 1 && v);
+    const int p = (int)rank - count(lo + 1);
+    const bool has = mine > lo;
+    const uint64_t all = __ballot(has);
+    const uint64_t chosen = __ballot(has && __builtin_popcountll(all & ((1ull << lane) - 1)) == p);
+    Seq s;
+    s.any = v && chosen;
+    const int b = s.any ? __builtin_ctzll(chosen) : 0;
+    s.begin = __builtin_amdgcn_readlane(from, b);
+    s.len = __builtin_amdgcn_readlane(len, b);
+    s.tile = REVERSE ? __builtin_amdgcn_readlane(mine, b) - 1 - lo : lo;
+    return s;
 }
 
 // O and lse of 128 queries, 32 a wave, over 64-key tiles in two LDS buffers (the next tile is loaded while
@@ -237,10 +282,10 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
                                                                              int64_t tiles) {
     constexpr int BN = HD <= 128 ? 64 : 32, NB = BN / 32;
     __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
-    int64_t slot;
+    int64_t rank;
     int h;
-    item_of(tiles, slot, h);
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
+    item_of(a.n_heads, rank, h);
+    const Seq sq = ranked_tile<BM, false>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
     const int kv = h / (a.n_heads / a.n_kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -345,10 +390,10 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     int64_t tiles) {
     constexpr int BN = HD <= 128 ? 64 : 32;
     __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
-    int64_t slot;
+    int64_t rank;
     int h;
-    item_of(tiles, slot, h);
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
+    item_of(a.n_heads, rank, h);
+    const Seq sq = ranked_tile<BM, false>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
     const int kv = h / (a.n_heads / a.n_kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -446,11 +491,11 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     __shared__ __attribute__((aligned(16))) uint16_t qd_lds[GROUPS][2][2][BQ * HD];
     __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][KL ? BM * HD : 8];
     __shared__ __attribute__((aligned(16))) float stat[GROUPS][2][2][BQ];  // lse in units of log 2, delta
-    int64_t slot;
+    int64_t rank;
     int kv;
-    item_of(tiles, slot, kv);
-    slot = tiles - 1 - slot;  // the first keys of a sequence are seen by the most queries
-    const Seq sq = find_tile<BM>(a.cu, a.n_seqs, a.T, slot);
+    item_of(a.n_kv, rank, kv);
+    // the first keys of a sequence are seen by the most queries
+    const Seq sq = ranked_tile<BM, true>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
     const int group = a.n_heads / a.n_kv;
     const int lane = threadIdx.x & 63, tid = threadIdx.x & 255;
