@@ -604,8 +604,10 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  * realq_packed_attention_backward: from dO, dQ (like q), dK and dV (like k, v; summed over the query
  * heads that share them), rows lddq / lddk / lddv apart, bf16, by the formulas
  *   dV = P^T dO,  dS = P (dO v^T - delta),  delta_i = sum O_i dO_i,  dQ = scale dS k,  dK = scale dS^T q;
- * O and lse as the forward call gave them; delta: [n_heads, T] float32 scratch.  The sums have a
- * fixed order: the same inputs give the same bits.  Outputs must not overlap inputs or each other
+ * O and lse as the forward call gave them; work: scratch memory of at least
+ * realq_packed_attention_workspace bytes (by T, n_seqs, the heads and head_dim; the arrays are not looked
+ * at), aligned to 16, which needs no clearing.  The sums have a fixed order: the same inputs give the same
+ * bits.  Outputs must not overlap inputs or each other
  * (rows of one wider array are fine).
  *
  * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
@@ -625,9 +627,11 @@ typedef struct realq_attention_desc {
 } realq_attention_desc;
 
 int realq_packed_attention(realq_ctx* ctx, const realq_attention_desc* desc, uint16_t* O, int64_t ldo, float* lse);
+int realq_packed_attention_workspace(realq_ctx* ctx, const realq_attention_desc* desc, size_t* bytes);
 int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* desc, const uint16_t* O, int64_t ldo,
-                                    const float* lse, const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ,
-                                    int64_t lddq, uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv);
+                                    const float* lse, const uint16_t* dO, int64_t lddo, void* work,
+                                    size_t work_bytes, uint16_t* dQ, int64_t lddq, uint16_t* dK, int64_t lddk,
+                                    uint16_t* dV, int64_t lddv);
 
 /* Product in 8-bit integers with a scale per token and per output channel: the hand-off of a module
  * quantized per row (realq_qparams.group = 0; its weights are codes - zeros with one scale per

@@ -15,6 +15,8 @@
 //
 // LDS tiles hold rows of HD channels in 16-byte chunks, chunk c of row r at c ^ f(r): 16 consecutive rows
 // read at one chunk, and 4 rows read at 4 chunks, each fall on distinct banks.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 
@@ -276,28 +278,34 @@ __device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64
 // maximum, sum and rescaling are the lane's own; only the maximum and the final sum cross to lane + 32.
 // O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
 // old one serves as well (P up to 256, exact to the same relative rounding).
-template <int HD>
-__global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a, uint16_t* __restrict__ O,
-                                                                             int64_t ldo, float* __restrict__ lse,
-                                                                             int64_t tiles) {
+template <int HD, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
+                                                                                       uint16_t* __restrict__ O,
+                                                                                       int64_t ldo,
+                                                                                       float* __restrict__ lse,
+                                                                                       int64_t tiles) {
     constexpr int BN = HD <= 128 ? 64 : 32, NB = BN / 32;
-    __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
+    __shared__ __attribute__((aligned(16))) uint16_t all_lds[GROUPS][2][2][BN * HD];
     int64_t rank;
     int h;
     item_of(a.n_heads, rank, h);
     const Seq sq = ranked_tile<BM, false>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
     const int kv = h / (a.n_heads / a.n_kv);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, tid = threadIdx.x & 255;
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = all >> 2, wave = all & 3;
+    uint16_t(*kv_lds)[2][BN * HD] = all_lds[grp];
     const int q0 = sq.tile * BM + wave * 32;           // this wave's first query, in the sequence
     const int qi = min(q0 + (lane & 31), sq.len - 1);  // this lane's
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
-    clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
-    const Loader<HD, BN, NT / 64> loader(a.hd, wave);
+    clear_rest<HD, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
+    const Loader<HD, BN, 4> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
-    loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
-    loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
+    if (grp * BN < keys) {
+        loader.load(K, a.ldk, grp * BN, sq.len, lds_at(kv_lds[0][0]));
+        loader.load(V, a.ldv, grp * BN, sq.len, lds_at(kv_lds[0][1]));
+    }
     bf16x8 qf[HD / 16];
     hold<HD>(a.q + (sq.begin + qi) * a.ldq + h * a.hd, a.hd, lane, qf);
     const float c = a.scale * kLog2e;
@@ -306,14 +314,15 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) o[t] = zero16();
     int buf = 0;
-    for (int k0 = 0; k0 < keys; k0 += BN, buf ^= 1) {
+    for (int k0 = grp * BN; k0 - grp * BN < keys; k0 += GROUPS * BN, buf ^= 1) {
         vm_wait<0>();
         block_sync();
-        if (k0 + BN < keys) {
-            loader.load(K, a.ldk, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][0]));
-            loader.load(V, a.ldv, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][1]));
+        const int next = k0 + GROUPS * BN;
+        if (next < keys) {
+            loader.load(K, a.ldk, next, sq.len, lds_at(kv_lds[buf ^ 1][0]));
+            loader.load(V, a.ldv, next, sq.len, lds_at(kv_lds[buf ^ 1][1]));
         }
-        if (k0 > q0 + 31) continue;
+        if (k0 > q0 + 31 || k0 >= keys) continue;  // nothing to see, or a later group's round past the last key
         const uint16_t* sk = kv_lds[buf][0];
         const uint16_t* sv = kv_lds[buf][1];
         f32x16 s[NB];
@@ -365,6 +374,29 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
             }
     }
     l += other_half(l);
+    if constexpr (GROUPS == 2) {  // both groups' sums on the larger maximum, through the LDS of the tiles
+        float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
+        static_assert(sizeof(all_lds) >= (HD / 2 + 2) * 256 * 4, "a thread's sums");
+        __syncthreads();
+        if (grp == 1) {
+            sh[0] = m;
+            sh[256] = l;
+#pragma unroll
+            for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sh[(2 + 16 * t + e) * 256] = o[t][e];
+        }
+        __syncthreads();
+        if (grp == 1) return;
+        const float m1 = sh[0], mn = fmaxf(m, m1);  // m is finite: every query sees the first tile's first key
+        const float f0 = __builtin_amdgcn_exp2f((m - mn) * c), f1 = __builtin_amdgcn_exp2f((m1 - mn) * c);
+        m = mn;
+        l = l * f0 + sh[256] * f1;
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] = o[t][e] * f0 + sh[(2 + 16 * t + e) * 256] * f1;
+    }
     if (q0 + (lane & 31) >= sq.len) return;
     const int64_t row = sq.begin + qi;
     const float inv = 1.f / l;
@@ -383,30 +415,42 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_forward_kernel(Att
 
 // dQ (and delta) of 128 queries, 32 a wave, over the key tiles they see, in two LDS buffers.  As in the
 // forward a query's scores are one lane's: S^T = K Q^T, dP^T = V dO^T, and dS^T goes into dQ^T += K^T dS^T.
-template <int HD>
-__global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
+// delta from the bf16 O is off by up to 2^-8 sum |O dO|, and dS is a small difference beside it where a softmax
+// has one large entry.  What it is off by is the sum of a row of dS (which is 0 for the true delta): that sum
+// goes into the delta stored for dK, and for the first tile of a sequence, whose rows see few keys (2 keys:
+// 6e-3 of dQ; 300: 2e-3), a pass over its keys forms delta as sum P dP first.
+template <int HD, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
     const uint16_t* __restrict__ dO, int64_t lddo, float* __restrict__ delta, uint16_t* __restrict__ dQ, int64_t lddq,
     int64_t tiles) {
     constexpr int BN = HD <= 128 ? 64 : 32;
-    __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][2][BN * HD];
+    __shared__ __attribute__((aligned(16))) uint16_t all_lds[GROUPS][2][2][BN * HD];
+    __shared__ float sums[GROUPS][BM];
     int64_t rank;
     int h;
     item_of(a.n_heads, rank, h);
     const Seq sq = ranked_tile<BM, false>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
     const int kv = h / (a.n_heads / a.n_kv);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, tid = threadIdx.x & 255;
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = all >> 2, wave = all & 3;
+    uint16_t(*kv_lds)[2][BN * HD] = all_lds[grp];
     const int q0 = sq.tile * BM + wave * 32;
     const int qi = min(q0 + (lane & 31), sq.len - 1);
     const int64_t row = sq.begin + qi;
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
-    clear_rest<HD, 4 * BN, NT>(kv_lds[0][0], a.hd);
-    const Loader<HD, BN, NT / 64> loader(a.hd, wave);
+    clear_rest<HD, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
+    const Loader<HD, BN, 4> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
-    loader.load(K, a.ldk, 0, sq.len, lds_at(kv_lds[0][0]));
-    loader.load(V, a.ldv, 0, sq.len, lds_at(kv_lds[0][1]));
+    auto begin = [&]() {
+        if (grp * BN < keys) {
+            loader.load(K, a.ldk, grp * BN, sq.len, lds_at(kv_lds[0][0]));
+            loader.load(V, a.ldv, grp * BN, sq.len, lds_at(kv_lds[0][1]));
+        }
+    };
+    begin();
     bf16x8 qf[HD / 16], df[HD / 16];
     hold<HD>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
     hold<HD>(dO + row * lddo + h * a.hd, a.hd, lane, df);
@@ -421,45 +465,89 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
         dl += other_half(dl);
     }
     const bool live = q0 + (lane & 31) < sq.len;
-    if (live && lane < 32) delta[(int64_t)h * a.T + row] = dl;
     const float c = a.scale * kLog2e, L = lse[(int64_t)h * a.T + row] * kLog2e;
     f32x16 g[HD / 32];
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) g[t] = zero16();
-    int buf = 0;
-    for (int k0 = 0; k0 < keys; k0 += BN, buf ^= 1) {
-        vm_wait<0>();
-        block_sync();
-        if (k0 + BN < keys) {
-            loader.load(K, a.ldk, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][0]));
-            loader.load(V, a.ldv, k0 + BN, sq.len, lds_at(kv_lds[buf ^ 1][1]));
-        }
-        const uint16_t* sk = kv_lds[buf][0];
-        const uint16_t* sv = kv_lds[buf][1];
-#pragma unroll
-        for (int b = 0; b < BN / 32; ++b) {
-            const int kb = k0 + 32 * b;
-            if (kb > q0 + 31) continue;
-            f32x16 s = zero16(), dp = zero16();
-#pragma unroll
-            for (int u = 0; u < HD / 16; ++u) {
-                s = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s);
-                dp = mfma(row_frag<HD>(sv, 32 * b, u, lane), df[u], dp);
+    float sum = 0.f;  // of this lane's part of the row of P dP, then of dS
+    auto sweep = [&](bool products) {
+        int buf = 0;
+        for (int k0 = grp * BN; k0 - grp * BN < keys; k0 += GROUPS * BN, buf ^= 1) {
+            vm_wait<0>();
+            block_sync();
+            const int next = k0 + GROUPS * BN;
+            if (next < keys) {
+                loader.load(K, a.ldk, next, sq.len, lds_at(kv_lds[buf ^ 1][0]));
+                loader.load(V, a.ldv, next, sq.len, lds_at(kv_lds[buf ^ 1][1]));
             }
-            order_reads<HD / 8, HD / 8, AHEAD>();
-            if (kb + 31 > q0)
+            const uint16_t* sk = kv_lds[buf][0];
+            const uint16_t* sv = kv_lds[buf][1];
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (kb + crow(e, lane) > qi) s[e] = -INFINITY;
+            for (int b = 0; b < BN / 32; ++b) {
+                const int kb = k0 + 32 * b;
+                if (kb > q0 + 31 || kb >= keys) continue;
+                f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
+                for (int u = 0; u < HD / 16; ++u) {
+                    s = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s);
+                    dp = mfma(row_frag<HD>(sv, 32 * b, u, lane), df[u], dp);
+                }
+                order_reads<HD / 8, HD / 8, AHEAD>();
+                if (kb + 31 > q0)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 d = pack_frag(s, x);
+                    for (int e = 0; e < 16; ++e)
+                        if (kb + crow(e, lane) > qi || qi == 0) s[e] = -INFINITY;  // one key: dS is 0
 #pragma unroll
-                for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
+                for (int e = 0; e < 16; ++e) {
+                    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
+                    sum += s[e];
+                }
+                if (!products) continue;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const bf16x8 d = pack_frag(s, x);
+#pragma unroll
+                    for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
+                }
             }
         }
+    };
+    // the sum over both halves of the wave and both groups, in every lane of the query
+    auto whole = [&]() {
+        float x = sum + other_half(sum);
+        sum = 0.f;
+        if constexpr (GROUPS == 2) {
+            if (lane < 32) sums[grp][wave * 32 + lane] = x;
+            __syncthreads();
+            x = sums[0][wave * 32 + (lane & 31)] + sums[1][wave * 32 + (lane & 31)];
+        }
+        __syncthreads();  // the tiles' LDS is free again
+        return x;
+    };
+    if (sq.tile == 0) {
+        dl = 0.f;
+        sweep(false);
+        dl = whole();
+        begin();
+    }
+    sweep(true);
+    const float off = whole();
+    if (live && grp == 0 && lane < 32) delta[(int64_t)h * a.T + row] = dl + off;
+    if constexpr (GROUPS == 2) {
+        float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
+        static_assert(sizeof(all_lds) >= HD / 2 * 256 * 4, "a thread's sums");
+        __syncthreads();
+        if (grp == 1)
+#pragma unroll
+            for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sh[(16 * t + e) * 256] = g[t][e];
+        __syncthreads();
+        if (grp == 1) return;
+#pragma unroll
+        for (int t = 0; t < HD / 32; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) g[t][e] += sh[(16 * t + e) * 256];
     }
     if (!live) return;
     uint16_t* out = dQ + row * lddq + h * a.hd;
@@ -481,12 +569,14 @@ __global__ __launch_bounds__(NT, HD <= 128 ? 2 : 1) void attn_dq_kernel(
 // its own, and their sums are added at the end in one order: a block of 8 waves puts two on a SIMD, one
 // multiplying while the other forms P and dS, without making the longest block (the first keys of a long
 // sequence, which sets the time) any longer.  KL: K is read from LDS, which leaves 8 waves of 128 channels
-// their 256 registers; DK, DV: what this launch forms (both, or one each where both do not fit).
+// their 256 registers; DK, DV: what this launch forms (both, or one each where both do not fit).  With splits > 1
+// a block takes one of that many shares of its tile's rounds and leaves float32 sums in `part`
+// ([split][dK, dV][T][n_kv hd]), which sum_splits_kernel adds in their order.
 template <int HD, int GROUPS, bool KL, bool DK, bool DV>
 __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
     const float* __restrict__ delta, uint16_t* __restrict__ dK, int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv,
-    int64_t tiles) {
+    int64_t tiles, int splits, float* __restrict__ part) {
     constexpr int BQ = 32, THREADS = 256 * GROUPS, ACC = HD / 32;
     __shared__ __attribute__((aligned(16))) uint16_t qd_lds[GROUPS][2][2][BQ * HD];
     __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][KL ? BM * HD : 8];
@@ -494,6 +584,8 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     int64_t rank;
     int kv;
     item_of(a.n_kv, rank, kv);
+    const int split = (int)(rank % splits);
+    rank /= splits;
     // the first keys of a sequence are seen by the most queries
     const Seq sq = ranked_tile<BM, true>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
@@ -520,7 +612,9 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
         if constexpr (DK) gk[t] = zero16();
         if constexpr (DV) gv[t] = zero16();
     }
-    const int first = sq.tile * BM, steps = (sq.len - first + BQ - 1) / BQ, total = steps * group;
+    const int first = sq.tile * BM, steps = (sq.len - first + BQ - 1) / BQ;
+    const int share = (steps * group + splits - 1) / splits, begin = min(split * share, steps * group);
+    const int total = min(begin + share, steps * group);  // this block's tiles: begin .. total - 1
     auto fetch = [&](int i, int buf, float& pl, float& pd) {  // tile i: its head and queries
         const int h = kv * group + i / steps, q = first + i % steps * BQ;
         loader.load(a.q + sq.begin * a.ldq + (int64_t)h * a.hd, a.ldq, q, sq.len, lds_at(qd_lds[grp][buf][0]));
@@ -538,12 +632,12 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
             if constexpr (DK) stat[grp][buf][1][tid] = pd;
         }
     };
-    if (grp < total) {
-        fetch(grp, 0, pl, pd);
+    if (begin + grp < total) {
+        fetch(begin + grp, 0, pl, pd);
         keep(0);
     }
     int buf = 0;
-    for (int i = grp; i - grp < total; i += GROUPS, buf ^= 1) {
+    for (int i = begin + grp; i - grp < total; i += GROUPS, buf ^= 1) {
         vm_wait<0>();
         __syncthreads();
         if (i >= total) break;  // the last round of the later groups; all waves have passed the same barriers
@@ -588,6 +682,7 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
                     if constexpr (DK) dp[4 * q + x] = s[4 * q + x] * (dp[4 * q + x] - d[x]);
                 }
             }
+            if (DK && qb == 0 && lane < 32) dp[0] = 0.f;  // a sequence's first query has one key: dS is 0
             const bf16x8 p[2] = {pack_frag(s, 0), pack_frag(s, 1)}, d[2] = {pack_frag(dp, 0), pack_frag(dp, 1)};
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -629,35 +724,87 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
             const int r = k0 + crow(e, lane), ch = 32 * t + (lane & 31);
             if (r >= sq.len || ch >= a.hd) continue;
             const int64_t at = sq.begin + r;
+            if (splits > 1) {
+                const int64_t one = a.T * a.n_kv * a.hd;
+                float* const p = part + 2 * split * one + (at * a.n_kv + kv) * a.hd + ch;
+                if constexpr (DK) p[0] = gk[t][e];
+                if constexpr (DV) p[one] = gv[t][e];
+                continue;
+            }
             if constexpr (DK) dK[at * lddk + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)(gk[t][e] * a.scale));
             if constexpr (DV) dV[at * lddv + kv * a.hd + ch] = __builtin_bit_cast(uint16_t, (__bf16)gv[t][e]);
         }
 }
 
-#define RQ_HEAD_DIM(KERNEL, GRID, ...)                                                              \
-    do {                                                                                            \
-        if (a.hd <= 64) hipLaunchKernelGGL(KERNEL<64>, GRID, dim3(NT), 0, st, __VA_ARGS__);         \
-        else if (a.hd <= 128) hipLaunchKernelGGL(KERNEL<128>, GRID, dim3(NT), 0, st, __VA_ARGS__);  \
-        else hipLaunchKernelGGL(KERNEL<256>, GRID, dim3(NT), 0, st, __VA_ARGS__);                   \
+// dK and dV from the splits' sums, 4 channels a thread; rows of the sequences only.
+__global__ __launch_bounds__(NT) void sum_splits_kernel(AttnArgs a, int splits, const float* __restrict__ part,
+                                                        uint16_t* __restrict__ dK, int64_t lddk,
+                                                        uint16_t* __restrict__ dV, int64_t lddv) {
+    const int64_t width = (int64_t)a.n_kv * a.hd, one = a.T * width;
+    const int64_t from = min(max((int64_t)a.cu[0], (int64_t)0), a.T), to = min((int64_t)a.cu[a.n_seqs], a.T);
+    for (int64_t i = ((int64_t)blockIdx.x * NT + threadIdx.x) * 4; i < 2 * one; i += (int64_t)gridDim.x * NT * 4) {
+        const bool v = i >= one;
+        const int64_t e = v ? i - one : i, row = e / width, ch = e - row * width;
+        if (row < from || row >= to) continue;
+        f32x4 x = *reinterpret_cast<const f32x4*>(part + i);
+        for (int s = 1; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(part + 2 * s * one + i);
+        if (!v) x *= a.scale;
+        *reinterpret_cast<u32x2*>(v ? dV + row * lddv + ch : dK + row * lddk + ch) =
+            u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    }
+}
+
+namespace {
+
+// Whether blocks of two wave groups serve: below 2.5 blocks of one group on each of 256 CUs the longest block sets
+// the time, and two groups shorten it (2048 tokens, 16 heads x 128, 272 blocks: forward 46 -> 37 us; 4096, 528
+// blocks: 102 -> 81 us); above, their common barriers and sums cost more (1088 blocks: 82 -> 93 us).
+bool two_groups(int64_t blocks) { return blocks < 640; }
+// Shares of a dK/dV tile's rounds, for about two blocks a CU: the first keys of a sequence would set the time
+// otherwise (backward of 2048 tokens, 32/8 heads x 128, 136 blocks: 286 us whole, 166 us in 4 shares, 191 us in
+// 8; 2 x 2048, 272 blocks: 342 us whole, 277 us in 2).  544 blocks are faster whole (512 against 560 us).
+int key_splits(const AttnArgs& a) {
+    const int64_t blocks = (a.T / BM + a.n_seqs) * a.n_kv;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(8, (512 + blocks / 2) / blocks));
+}
+
+}  // namespace
+
+#define RQ_HEAD_DIM(KERNEL, BLOCKS, ...)                                                                              \
+    do {                                                                                                              \
+        const dim3 g_((unsigned)(BLOCKS));                                                                            \
+        if (a.hd > 128) hipLaunchKernelGGL((KERNEL<256, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                      \
+        else if (two_groups(BLOCKS) && a.hd <= 64) hipLaunchKernelGGL((KERNEL<64, 2>), g_, dim3(512), 0, st, __VA_ARGS__);   \
+        else if (two_groups(BLOCKS)) hipLaunchKernelGGL((KERNEL<128, 2>), g_, dim3(512), 0, st, __VA_ARGS__);         \
+        else if (a.hd <= 64) hipLaunchKernelGGL((KERNEL<64, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                  \
+        else hipLaunchKernelGGL((KERNEL<128, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                                 \
     } while (0)
 
 hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st) {
     const int64_t tiles = a.T / BM + a.n_seqs;
-    const dim3 grid((unsigned)(tiles * a.n_heads));
-    RQ_HEAD_DIM(attn_forward_kernel, grid, a, O, ldo, lse, tiles);
+    RQ_HEAD_DIM(attn_forward_kernel, tiles * a.n_heads, a, O, ldo, lse, tiles);
     return hipGetLastError();
 }
 
+size_t attn_packed_workspace(const AttnArgs& a) {
+    const int splits = key_splits(a);
+    const int64_t delta = (a.n_heads * a.T + 3) / 4 * 4;  // the splits' sums start on 16 bytes
+    return (size_t)(delta + (splits > 1 ? 2 * splits * a.T * a.n_kv * a.hd : 0)) * 4;
+}
+
 hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ldo, const float* lse,
-                                const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ, int64_t lddq,
-                                uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st) {
+                                const uint16_t* dO, int64_t lddo, void* work, uint16_t* dQ, int64_t lddq, uint16_t* dK,
+                                int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st) {
     const int64_t tiles = a.T / BM + a.n_seqs;
-    const dim3 gq((unsigned)(tiles * a.n_heads)), gk((unsigned)(tiles * a.n_kv));
-    RQ_HEAD_DIM(attn_dq_kernel, gq, a, O, ldo, lse, dO, lddo, delta, dQ, lddq, tiles);
+    float* const delta = (float*)work;
+    RQ_HEAD_DIM(attn_dq_kernel, tiles * a.n_heads, a, O, ldo, lse, dO, lddo, delta, dQ, lddq, tiles);
     if (const hipError_t e = hipGetLastError()) return e;
-#define RQ_DKV(HD, GROUPS, KL, DK, DV)                                                                             \
-    hipLaunchKernelGGL((attn_dkv_kernel<HD, GROUPS, KL, DK, DV>), gk, dim3(256 * GROUPS), 0, st, a, lse, dO, lddo, \
-                       delta, dK, lddk, dV, lddv, tiles)
+    const int splits = key_splits(a);
+    float* const part = delta + (a.n_heads * a.T + 3) / 4 * 4;
+    const dim3 grid((unsigned)(tiles * a.n_kv * splits));
+#define RQ_DKV(HD, GROUPS, KL, DK, DV)                                                                               \
+    hipLaunchKernelGGL((attn_dkv_kernel<HD, GROUPS, KL, DK, DV>), grid, dim3(256 * GROUPS), 0, st, a, lse, dO, lddo, \
+                       delta, dK, lddk, dV, lddv, tiles, splits, part)
     if (a.hd <= 64) {
         RQ_DKV(64, 2, false, true, true);
     } else if (a.hd <= 128) {
@@ -667,6 +814,12 @@ hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ld
         RQ_DKV(256, 1, false, true, false);
     }
 #undef RQ_DKV
+    if (splits > 1) {
+        if (const hipError_t e = hipGetLastError()) return e;
+        const int64_t quads = 2 * a.T * a.n_kv * a.hd / 4;
+        hipLaunchKernelGGL(sum_splits_kernel, dim3((unsigned)std::min<int64_t>((quads + NT - 1) / NT, 1 << 16)), dim3(NT),
+                           0, st, a, splits, part, dK, lddk, dV, lddv);
+    }
     return hipGetLastError();
 }
 

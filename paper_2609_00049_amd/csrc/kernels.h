@@ -355,9 +355,9 @@ struct AttnArgs {
     float scale;
 };
 hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st);
-// delta: [n_heads][T] workspace
+size_t attn_packed_workspace(const AttnArgs& a);  // of the backward
 hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ldo, const float* lse,
-                                const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ, int64_t lddq,
-                                uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st);
+                                const uint16_t* dO, int64_t lddo, void* work, uint16_t* dQ, int64_t lddq, uint16_t* dK,
+                                int64_t lddk, uint16_t* dV, int64_t lddv, hipStream_t st);
 
 }  // namespace realq

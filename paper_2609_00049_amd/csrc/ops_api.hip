@@ -190,9 +190,19 @@ int realq_packed_attention(realq_ctx* ctx, const realq_attention_desc* d, uint16
     });
 }
 
+int realq_packed_attention_workspace(realq_ctx* ctx, const realq_attention_desc* d, size_t* bytes) {
+    return guarded(ctx, [&]() -> int {
+        if (const int rc = check_attention(ctx, d, "packed_attention_workspace")) return rc;
+        if (!bytes) return set_error(ctx, REALQ_ERR_INVALID_ARG, "packed_attention_workspace: NULL bytes");
+        *bytes = d->T == 0 || d->n_seqs == 0 ? 0 : realq::attn_packed_workspace(attn_args(d));
+        return REALQ_OK;
+    });
+}
+
 int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* d, const uint16_t* O, int64_t ldo,
-                                    const float* lse, const uint16_t* dO, int64_t lddo, float* delta, uint16_t* dQ,
-                                    int64_t lddq, uint16_t* dK, int64_t lddk, uint16_t* dV, int64_t lddv) {
+                                    const float* lse, const uint16_t* dO, int64_t lddo, void* work,
+                                    size_t work_bytes, uint16_t* dQ, int64_t lddq, uint16_t* dK, int64_t lddk,
+                                    uint16_t* dV, int64_t lddv) {
     return guarded(ctx, [&]() -> int {
         const char* who = "packed_attention_backward";
         if (const int rc = check_attention(ctx, d, who)) return rc;
@@ -204,12 +214,16 @@ int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* 
         if (const int rc = check_heads(ctx, who, "dQ", dQ, lddq, H, hd)) return rc;
         if (const int rc = check_heads(ctx, who, "dK", dK, lddk, G, hd)) return rc;
         if (const int rc = check_heads(ctx, who, "dV", dV, lddv, G, hd)) return rc;
-        if (!lse || !delta || !aligned(lse, 4) || !aligned(delta, 4))
-            return set_error(ctx, REALQ_ERR_INVALID_ARG, "packed_attention_backward: lse or delta is NULL or not aligned");
+        if (!lse || !aligned(lse, 4))
+            return set_error(ctx, REALQ_ERR_INVALID_ARG, "packed_attention_backward: lse is NULL or not aligned");
+        const size_t need = realq::attn_packed_workspace(attn_args(d));
+        if (!work || !aligned(work, 16) || work_bytes < need)
+            return set_error(ctx, REALQ_ERR_INVALID_ARG,
+                             "packed_attention_backward: the workspace needs " + std::to_string(need) + " bytes on 16");
         OnDevice on;
         RQ_HIP(ctx, on.enter(ctx->device));
         Timed tm(ctx, "packed_attention");
-        RQ_HIP(ctx, realq::attn_packed_backward(attn_args(d), O, ldo, lse, dO, lddo, delta, dQ, lddq, dK, lddk, dV,
+        RQ_HIP(ctx, realq::attn_packed_backward(attn_args(d), O, ldo, lse, dO, lddo, work, dQ, lddq, dK, lddk, dV,
                                                 lddv, ctx->stream));
         return REALQ_OK;
     });

@@ -39,7 +39,7 @@ EXPORTS = [
     "realq_pullback_metric", "realq_handoff", "realq_mlp_block_sweep",
     "realq_decoder_block_sweep", "realq_decoder_forward", "realq_mfma_peak",
     "realq_token_logprobs_workspace", "realq_token_logprobs", "realq_token_logprobs_backward",
-    "realq_packed_attention", "realq_packed_attention_backward",
+    "realq_packed_attention", "realq_packed_attention_workspace", "realq_packed_attention_backward",
     "realq_quantize_rows_i8", "realq_linear_i8",
 ]
 
@@ -186,8 +186,10 @@ def _load():
         "realq_token_logprobs_backward": (ctypes.c_int, [vp, ctypes.POINTER(LogprobsDesc), vp, vp, vp, vp, vp, vp, vp,
                                                          i64]),
         "realq_packed_attention": (ctypes.c_int, [vp, ctypes.POINTER(AttentionDesc), vp, i64, vp]),
+        "realq_packed_attention_workspace": (ctypes.c_int, [vp, ctypes.POINTER(AttentionDesc),
+                                                            ctypes.POINTER(ctypes.c_size_t)]),
         "realq_packed_attention_backward": (ctypes.c_int, [vp, ctypes.POINTER(AttentionDesc), vp, i64, vp, vp, i64, vp,
-                                                           vp, i64, vp, i64, vp, i64]),
+                                                           ctypes.c_size_t, vp, i64, vp, i64, vp, i64]),
         "realq_quantize_rows_i8": (ctypes.c_int, [vp, vp, i32, i64, i64, i64, vp, i64, vp]),
         "realq_linear_i8": (ctypes.c_int, [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i32, i64]),
     }
@@ -825,9 +827,11 @@ def packed_attention_backward(ctx: Context, q, k, v, cu_seqlens, out, lse, dout,
     dq = call.new(q.shape, BF16) if dq is None else dq
     dk = call.new(k.shape, BF16) if dk is None else dk
     dv = call.new(v.shape, BF16) if dv is None else dv
-    delta = call.new((desc.n_heads, desc.T), F32)
+    ref, need = ctypes.byref(desc), ctypes.c_size_t()
+    ctx.check(_lib.realq_packed_attention_workspace(ctx.h, ref, ctypes.byref(need)))
+    work = call.new((need.value,), U8)
     ctx.check(_lib.realq_packed_attention_backward(
-        ctx.h, ctypes.byref(desc), o, ldo, pl, d, lddo, delta.data_ptr(), *call.rows(dq, "dq", _BF, q.shape),
+        ctx.h, ref, o, ldo, pl, d, lddo, work.data_ptr(), need.value, *call.rows(dq, "dq", _BF, q.shape),
         *call.rows(dk, "dk", _BF, k.shape), *call.rows(dv, "dv", _BF, v.shape)))
     return dq, dk, dv
 

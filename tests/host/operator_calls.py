@@ -110,9 +110,10 @@ def attention(L):
         return ctypes.byref(d), o, ldo, lse
 
     def bwd(d, **kw):
-        a = dict(O=buf(5), ldo=512, lse=buf(6), dO=buf(7), lddo=512, delta=buf(8), dQ=buf(9), lddq=512, dK=buf(10),
+        a = dict(O=buf(5), ldo=512, lse=buf(6), dO=buf(7), lddo=512, work=buf(8), size=1 << 40, dQ=buf(9), lddq=512, dK=buf(10),
                  lddk=128, dV=buf(11), lddv=128)
         a.update(kw)
+        a["size"] = ctypes.c_size_t(a["size"])
         return (ctypes.byref(d), *a.values())
     assert launched(L, f, *fwd(desc())) >= 1 and launched(L, f, *fwd(desc(), lse=None)) >= 1
     assert launched(L, g, *bwd(desc())) >= 1
@@ -129,12 +130,24 @@ def attention(L):
         refused(L, code, "packed_attention_backward", g, *bwd(desc(**kw)))
     for kw, code in ((dict(o=None), -1), (dict(o=at(buf(5), 8)), -1), (dict(ldo=504), -2), (dict(lse=at(buf(6), 2)), -1)):
         refused(L, code, "packed_attention", f, *fwd(desc(), **kw))
-    for kw, code in ((dict(O=None), -1), (dict(lse=None), -1), (dict(delta=None), -1), (dict(dO=None), -1),
+    for kw, code in ((dict(O=None), -1), (dict(lse=None), -1), (dict(work=None), -1), (dict(work=at(buf(8), 8)), -1), (dict(size=10), -1), (dict(dO=None), -1),
                      (dict(dQ=None), -1), (dict(dK=None), -1), (dict(dV=None), -1), (dict(lddq=508), -2),
                      (dict(lddk=120), -2), (dict(dV=at(buf(11), 2)), -1)):
         refused(L, code, "packed_attention_backward", g, *bwd(desc(), **kw))
     refused(L, -2, "2^23", f, *fwd(desc(T=1 << 28, n_seqs=1 << 10)))
     refused(L, -2, "2^24", f, *fwd(desc(ldq=(1 << 24) + 8)))
+    h = "realq_packed_attention_workspace"
+    n = ctypes.c_size_t()
+    for kw in (dict(), dict(T=1), dict(T=4097, n_seqs=1), dict(T=100000), dict(n_heads=2, n_kv=1)):
+        d = desc(**kw)
+        L.ok(h, ctypes.byref(d), ctypes.byref(n))
+        assert n.value >= 4 * d.T * d.n_heads
+        assert launched(L, g, *bwd(d, size=n.value)) >= 1
+        refused(L, -1, str(n.value), g, *bwd(d, size=n.value - 1))
+    L.ok(h, ctypes.byref(desc(T=0, q=None, cu_seqlens=None)), ctypes.byref(n))
+    assert n.value == 0
+    refused(L, -1, "NULL", h, ctypes.byref(desc()), None)
+    refused(L, -2, "head_dim", h, ctypes.byref(desc(head_dim=7)), ctypes.byref(n))
     for hd in (8, 64, 128, 256):
         big = desc(T=(1 << 27) - 128, n_seqs=1, head_dim=hd, ldq=8 * hd, ldk=2 * hd, ldv=2 * hd)
         assert launched(L, f, *fwd(big, ldo=8 * hd)) >= 1

@@ -119,6 +119,28 @@ def test_strided_rows(rq, ctx):
     assert (grads[:, w:] == 3).all()
 
 
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_a_single_key_has_no_gradient(rq, ctx, hd):
+    """The softmax over one key is constant: dQ of every sequence's first token and dK of sequences of one
+    token are 0, to the bit."""
+    q, k, v, do, cu = make([1, 40, 1, 1, 200], 4, 2, hd, 11)
+    o, lse = rq.packed_attention(ctx, q, k, v, cu)
+    dq, dk, dv = rq.packed_attention_backward(ctx, q, k, v, cu, o, lse, do)
+    assert (dq[cu[:-1].long()] == 0).all() and (dk[[0, 41, 42]] == 0).all()
+    assert torch.equal(o[0], v[0].repeat_interleave(2, 0)) and (dk[1] != 0).any()
+
+
+def test_peaked_rows_keep_their_gradient(rq, ctx):
+    """Few keys and saturated rows, where dS is a small difference: relative to its 2-norm dQ and dK keep the
+    roundings of dS and of the output (each 2^-8 at most, evenly spread: 2^-8 / sqrt(3)), within a factor of 2."""
+    q, k, v, do, cu = make([2] * 40 + [5] * 20 + [17] * 6, 4, 2, 96, 12)
+    o, lse = rq.packed_attention(ctx, q, k, v, cu)
+    want = ref.attention(q, k, v, cu, do)
+    for name, got in zip(("dq", "dk"), rq.packed_attention_backward(ctx, q, k, v, cu, o, lse, do)):
+        off = (got.double() - want[name][0]).norm() / want[name][0].norm()
+        assert off <= 2 * math.sqrt(2 / 3) * ref.BF, (name, float(off))
+
+
 def test_gradients_against_differences(rq, ctx):
     """The gradients along a direction against central differences of the float64 definition."""
     q, k, v, do, cu = make([45, 20], 4, 2, 64, 7)

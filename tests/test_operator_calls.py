@@ -40,7 +40,8 @@ def test_null_contexts():
     assert lib.realq_token_logprobs(None, None, z, z, z, z, z, z, 0) == -1
     assert lib.realq_token_logprobs_backward(None, None, z, z, z, z, z, z, z, 0) == -1
     assert lib.realq_packed_attention(None, None, z, 0, z) == -1
-    assert lib.realq_packed_attention_backward(None, None, z, 0, z, z, 0, z, z, 0, z, 0, z, 0) == -1
+    assert lib.realq_packed_attention_workspace(None, None, None) == -1
+    assert lib.realq_packed_attention_backward(None, None, z, 0, z, z, 0, z, 0, z, 0, z, 0, z, 0) == -1
     assert lib.realq_quantize_rows_i8(None, z, 0, 0, 0, 0, z, 0, z) == -1
     assert lib.realq_linear_i8(None, z, 0, z, z, 0, z, z, 0, 0, 0, z, 0, 0) == -1
 
