@@ -154,19 +154,19 @@ constexpr int CAP = 1024;  // candidates kept in LDS
 
 // A block scans one of S stretches of a row: 4 vectors a thread in flight, one rebase of the running
 // sums per 4 vectors.  The alternatives cost the scan two operations per 4 vectors (the largest value a
-// thread has seen and where): a group of 4 threads gives one key that some element of theirs reaches, so
+// thread has seen and where): a 64th of the threads gives one key that some element of theirs reaches, so
 // the top-th largest of the 64 keys bounds the alternatives from below, and only the threads whose
 // largest value passes that bound (about `top` of them) have their vectors, by now in the L2, read again,
 // a wave on each.  What passes is ranked by counting.  Keys are distinct, so ties cannot fill the list;
 // should more than CAP elements pass (or fewer than top: NaN), the stretch is searched once per alternative.
 // S == 1 writes the results; else the sums and keys go to `work`, and merge_kernel joins them.
-template <class E, bool TOP>
-__global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64_t T, int64_t V, int64_t ld, int S,
+template <class E, int BT, bool TOP>
+__global__ __launch_bounds__(BT) void scan_kernel(const E* __restrict__ Z, int64_t T, int64_t V, int64_t ld, int S,
                                                   int top, Out out, Acc4* __restrict__ part,
                                                   uint64_t* __restrict__ keys) {
     using R = Row<E>;
     constexpr int N = R::N, U = 4;
-    __shared__ Acc wacc[NT / 64];
+    __shared__ Acc wacc[BT / 64];
     __shared__ uint64_t group[64], cand[TOP ? CAP : 1];
     __shared__ uint64_t bound;
     __shared__ int count;
@@ -215,10 +215,10 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
             a.u += w;
         };
         int64_t v = v0 + tid;
-        for (; v + (U - 1) * NT < v1; v += U * NT) {
+        for (; v + (U - 1) * BT < v1; v += U * BT) {
             u32x4 x[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = row.load(v + u * NT);
+            for (int u = 0; u < U; ++u) x[u] = row.load(v + u * BT);
             take(x, v);
         }
         if (v < v1) {
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
             for (int u = 0; u < U; ++u) {
                 const uint32_t none = sizeof(E) == 2 ? 0xFF80FF80u : 0xFF800000u;  // -infinity
                 x[u] = u32x4{none, none, none, none};
-                if (v + u * NT < v1) x[u] = row.load(v + u * NT);
+                if (v + u * BT < v1) x[u] = row.load(v + u * BT);
             }
             take(x, v);
         }
@@ -237,10 +237,10 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
         if constexpr (TOP) {
             // a key no larger than that of some element of this thread: its largest value at the last
             // column it could have in its 4 vectors
-            uint64_t k = bv < 0 ? 0 : key_of(bm, min(row.column(bv + (U - 1) * NT) + N - 1, V - 1));
-            k = max(k, (uint64_t)__shfl_xor((unsigned long long)k, 1));
-            k = max(k, (uint64_t)__shfl_xor((unsigned long long)k, 2));
-            if ((tid & 3) == 0) group[tid >> 2] = k;
+            uint64_t k = bv < 0 ? 0 : key_of(bm, min(row.column(bv + (U - 1) * BT) + N - 1, V - 1));
+#pragma unroll
+            for (int w = 1; w < BT / 64; w *= 2) k = max(k, (uint64_t)__shfl_xor((unsigned long long)k, w));
+            if (tid % (BT / 64) == 0) group[tid / (BT / 64)] = k;
             if (tid == 0) {
                 count = 0;
                 bound = 1;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
         }
         __syncthreads();
         if (tid == 0) {
-            for (int w = 1; w < NT / 64; ++w) merge(a, wacc[w]);
+            for (int w = 1; w < BT / 64; ++w) merge(a, wacc[w]);
             if (S == 1) row_lse = finish(a, row.z, V, t, out);
             else part[item] = {a.m, a.s, a.u, 0.f};
         }
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
             while (again) {
                 const int src = __builtin_ctzll(again);
                 again &= again - 1;
-                for (int64_t w = v0 + wave * 64 + src + (int64_t)lane * NT; w < v1; w += 64 * NT) {
+                for (int64_t w = v0 + wave * 64 + src + (int64_t)lane * BT; w < v1; w += 64 * BT) {
                     float f[N];
                     unpack(row.load(w), f, E());
 #pragma unroll
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
                 else mine[r] = k;
             };
             if (c <= CAP && c >= want) {
-                for (int i = tid; i < c; i += NT) {
+                for (int i = tid; i < c; i += BT) {
                     const uint64_t k = cand[i];
                     int r = 0;
                     for (int x = 0; x < c; ++x) r += cand[x] > k;
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
                         const uint64_t k = key_of(z, j);
                         if (k < last && k > b) b = k;
                     };
-                    for (int64_t w = v0 + tid; w < v1; w += NT) {
+                    for (int64_t w = v0 + tid; w < v1; w += BT) {
                         float f[N];
                         unpack(row.load(w), f, E());
 #pragma unroll
@@ -320,13 +320,13 @@ __global__ __launch_bounds__(NT) void scan_kernel(const E* __restrict__ Z, int64
                     __syncthreads();
                     if (lane == 0) group[wave] = b;
                     __syncthreads();
-                    for (int w = 0; w < NT / 64; ++w) b = max(b, group[w]);
+                    for (int w = 0; w < BT / 64; ++w) b = max(b, group[w]);
                     last = b;
                     if (tid == 0) emit(b, r);
                 }
             }
             if (S > 1)
-                for (int r = want + tid; r < top; r += NT) mine[r] = 0;
+                for (int r = want + tid; r < top; r += BT) mine[r] = 0;
         }
         __syncthreads();
     }
@@ -459,12 +459,13 @@ __global__ __launch_bounds__(NT) void backward_kernel(const E* Z, int64_t T, int
 
 namespace {
 
-// Stretches of a row: one where the rows alone are two blocks a CU (measured on 256 CUs: see the launch
-// below), else enough for four, of 4 KB at least and 64 (the lanes of the joining wave) at most.
+// Stretches of a row: one up to 1 MiB (a block of 1024 threads has a row of 128256 bf16 in the time that the
+// second launch alone would take), else of 64 KiB or more, enough for four blocks a CU, 64 (the lanes of the
+// joining wave) at most.
 int stretches(int64_t T, int64_t V, bool f32, int cus) {
-    if (T >= 2 * cus) return 1;
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(64, V * (f32 ? 4 : 2) / 4096));
-    return (int)std::min<int64_t>(most, (4 * cus + T - 1) / T);
+    const int64_t bytes = V * (f32 ? 4 : 2);
+    if (bytes <= 1 << 20 || T >= 4 * cus) return 1;
+    return (int)std::min<int64_t>(std::min<int64_t>(64, bytes >> 16), (4 * cus + T - 1) / T);
 }
 constexpr int64_t kMostBlocks = 1 << 20;  // a launch holds fewer than 2^32 threads; the kernels loop
 
@@ -483,8 +484,15 @@ static hipError_t forward(const LogprobsArgs& a, const Out& o, void* work, int c
     uint64_t* keys = S == 1 ? nullptr : (uint64_t*)(part + a.T * S);
     const dim3 grid((unsigned)std::min<int64_t>(a.T * S, kMostBlocks));
     const E* z = (const E*)a.logits;
-    if (a.top) hipLaunchKernelGGL((scan_kernel<E, true>), grid, dim3(NT), 0, st, z, a.T, a.V, a.ld, S, a.top, o, part, keys);
-    else hipLaunchKernelGGL((scan_kernel<E, false>), grid, dim3(NT), 0, st, z, a.T, a.V, a.ld, S, 0, o, part, keys);
+#define RQ_SCAN(BT, TOP) \
+    hipLaunchKernelGGL((scan_kernel<E, BT, TOP>), grid, dim3(BT), 0, st, z, a.T, a.V, a.ld, S, a.top, o, part, keys)
+    // Few blocks: 16 waves each, for their loads in flight; many: 4, which start and end at more different times.
+    const bool few = a.T * S < 2 * cus;
+    if (few && a.top) RQ_SCAN(1024, true);
+    else if (few) RQ_SCAN(1024, false);
+    else if (a.top) RQ_SCAN(256, true);
+    else RQ_SCAN(256, false);
+#undef RQ_SCAN
     if (S > 1) {
         if (const hipError_t e = hipGetLastError()) return e;
         hipLaunchKernelGGL(merge_kernel<E>, dim3((unsigned)std::min<int64_t>(a.T, kMostBlocks)), dim3(64),

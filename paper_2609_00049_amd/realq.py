@@ -680,45 +680,44 @@ class _Call:
         # another stream is current: memory of the call must not be given out again, nor made, on that one
         self.foreign = _current(ctx.device.index) != ctx.raw_stream
 
-    def use(self, t: torch.Tensor, name: str) -> int:
-        if t.device != self.device:
-            raise ValueError(f"{name} must be on {self.device}, got {t.device}")
-        if self.foreign:
-            t.record_stream(self.ctx.stream)
-        return t.data_ptr()
-
-    @staticmethod
-    def check(t, name: str, dtypes, shape):
+    def rows(self, t, name: str, dtypes, shape):
+        """(address, elements between rows) of a tensor whose rows (the axes after the first) are contiguous."""
         if not isinstance(t, torch.Tensor):
             raise ValueError(f"{name} must be a torch.Tensor")
         if t.dtype not in dtypes:
             raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
         if t.shape != shape:
             raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.is_contiguous():
+            ld = shape[1] if len(shape) == 2 else math.prod(shape[1:])
+        else:
+            ld = self._stride(t, name)
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device}, got {t.device}")
+        if self.foreign:
+            t.record_stream(self.ctx.stream)
+        return t.data_ptr(), ld
+
+    @staticmethod
+    def _stride(t, name: str) -> int:
+        width = 1
+        for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+            if size > 1 and stride != width:
+                raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
+            width *= size
+        if t.shape[0] == 1:
+            return width
+        if t.stride(0) < width:
+            raise ValueError(f"the rows of {name} overlap: strides {t.stride()}")
+        return t.stride(0)
 
     def flat(self, t, name: str, dtypes, shape):
         """Address of a contiguous tensor, or None."""
         if t is None:
             return None
-        self.check(t, name, dtypes, shape)
-        if not t.is_contiguous():
+        if isinstance(t, torch.Tensor) and not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-        return self.use(t, name)
-
-    def rows(self, t, name: str, dtypes, shape):
-        """(address, elements between rows) of a tensor whose rows (the axes after the first) are contiguous."""
-        self.check(t, name, dtypes, shape)
-        if not t.is_contiguous():
-            width = 1
-            for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-                if size > 1 and stride != width:
-                    raise ValueError(f"the rows of {name} must be contiguous, got strides {t.stride()}")
-                width *= size
-            if t.shape[0] > 1:
-                if t.stride(0) < width:
-                    raise ValueError(f"the rows of {name} overlap: strides {t.stride()}")
-                return self.use(t, name), t.stride(0)
-        return self.use(t, name), math.prod(shape[1:])
+        return self.rows(t, name, dtypes, shape)[0]
 
     def new(self, shape, dtype) -> torch.Tensor:
         if not self.foreign:
@@ -808,8 +807,11 @@ def packed_attention(ctx: Context, q, k, v, cu_seqlens, *, scale: Optional[float
     1 / sqrt(head_dim) by default."""
     call = _Call(ctx)
     desc = _attention_desc(call, q, k, v, cu_seqlens, scale)
-    out = call.new(q.shape, BF16) if out is None else out
-    o, ldo = call.rows(out, "out", _BF, q.shape)
+    if out is None:
+        out = call.new(q.shape, BF16)
+        o, ldo = out.data_ptr(), desc.n_heads * desc.head_dim
+    else:
+        o, ldo = call.rows(out, "out", _BF, q.shape)
     lse = call.new((desc.n_heads, desc.T), F32)
     ctx.check(_lib.realq_packed_attention(ctx.h, ctypes.byref(desc), o, ldo, lse.data_ptr()))
     return out, lse
@@ -843,10 +845,13 @@ def quantize_rows_i8(ctx: Context, X, out=None):
     call = _Call(ctx)
     x, ldx = call.rows(X, "X", _FLOAT, (T, n))
     if out is None:
-        out = call.new((T, -(-n // 16) * 16), I8)
-        if n % 16:
+        ldq = -(-n // 16) * 16
+        out = call.new((T, ldq), I8)
+        q = out.data_ptr()
+        if ldq != n:
             out = out[:, :n]
-    q, ldq = call.rows(out, "out", _I8, (T, n))
+    else:
+        q, ldq = call.rows(out, "out", _I8, (T, n))
     s = call.new((T,), F32)
     ctx.check(_lib.realq_quantize_rows_i8(ctx.h, x, _DTYPE[X.dtype], T, n, ldx, q, ldq, s.data_ptr()))
     return out, s
@@ -865,7 +870,9 @@ def linear_i8(ctx: Context, Xq, sx, Wq, sw, *, bias=None, dtype=torch.bfloat16, 
         if dtype not in _DTYPE:
             raise ValueError(f"dtype must be torch.bfloat16 or torch.float32, got {dtype}")
         out = call.new((T, m), dtype)
-    y, ldy = call.rows(out, "out", _FLOAT, (T, m))
+        y, ldy = out.data_ptr(), m
+    else:
+        y, ldy = call.rows(out, "out", _FLOAT, (T, m))
     ctx.check(_lib.realq_linear_i8(ctx.h, x, ldx, call.flat(sx, "sx", _F, (T,)), w, ldw, call.flat(sw, "sw", _F, (m,)),
                                    call.flat(bias, "bias", _F, (m,)), T, n, m, y, _DTYPE[out.dtype], ldy))
     return out

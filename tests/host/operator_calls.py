@@ -68,12 +68,12 @@ def logprobs(L):
                dict(work=at(buf(8), 8))):
         refused(L, -1, "token_logprobs", f, *args(desc(), **kw))
     assert work_for(L, desc(T=0)) == 0
-    few = desc(T=1, V=200000, ld=200000)
+    few = desc(T=1, V=2000000, ld=2000000)
     need = work_for(L, few)
-    if need:
-        refused(L, -1, str(need), f, *args(few, size=need - 1))
-        refused(L, -1, str(need), f, *args(few, work=None))
-        assert launched(L, f, *args(few, size=need)) >= 1
+    assert need > 0
+    refused(L, -1, str(need), f, *args(few, size=need - 1))
+    refused(L, -1, str(need), f, *args(few, work=None))
+    assert launched(L, f, *args(few, size=need)) >= 1
     # many rows: launch limits (a grid dimension times its block below 2^32)
     for T, V in ((1 << 24, 8), (1 << 33, 4), (1, (1 << 31) - 1), (40, (1 << 31) - 1)):
         d = desc(T=T, V=V, ld=V, top=2)

@@ -8,7 +8,7 @@ from tests import operator_reference as ref
 
 pytestmark = pytest.mark.gpu
 
-SIZES = [(1, 1), (1, 7), (3, 64), (2, 1000), (5, 4099), (33, 32003), (1, 128256), (257, 2051), (600, 515), (40, 151936)]
+SIZES = [(1, 1), (1, 7), (3, 64), (2, 1000), (5, 4099), (33, 32003), (1, 128256), (257, 2051), (600, 515), (40, 151936), (1, 700001), (3, 1100003)]
 
 
 def make(T, V, dtype, seed=0):
