@@ -499,21 +499,23 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
 }
 
 // ---------------------------------------------------------------- few tokens: the weights are read once
-// A block takes 16 weight rows and its waves a share of the columns each, 128 at a time (a row's whole line),
+// A block takes 16 RT weight rows and its waves a share of the columns each, 128 at a time (a row's whole line),
 // straight from memory into the operand layout of v_mfma_i32_16x16x64_i8: lane l holds 16 columns of row
 // l % 16, and of token l % 16.  The waves' integer sums meet in LDS.
-template <int TT, class E>
+template <int TT, int RT, class E>
 __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __restrict__ W, int64_t ldw,
                                                             const int8_t* __restrict__ X, int64_t ldx, int64_t m,
                                                             int64_t T, int64_t n, const float* __restrict__ sx,
                                                             const float* __restrict__ sw,
                                                             const float* __restrict__ bias, E* __restrict__ Y,
                                                             int64_t ldy) {
-    constexpr int NW = 8, U = TT <= 2 ? 4 : 2;  // steps of 128 columns under way in a wave
-    __shared__ int32_t part[NW][TT * 256];
+    constexpr int NW = 8, U = TT * RT <= 2 ? 4 : 2;  // steps of 128 columns under way in a wave
+    __shared__ int32_t part[NW][TT * RT * 256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i0 = (int64_t)blockIdx.x * 16;
-    const int8_t* w = W + min(i0 + (lane & 15), m - 1) * ldw;
+    const int64_t i0 = (int64_t)blockIdx.x * (16 * RT);
+    const int8_t* w[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) w[r] = W + min(i0 + 16 * r + (lane & 15), m - 1) * ldw;
     const int8_t* x[TT];
     bool here[TT];
 #pragma unroll
@@ -532,21 +534,24 @@ __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __rest
         }
         return v;
     };
-    i32x4 acc[TT];
+    i32x4 acc[RT][TT];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[r][t] = i32x4{0, 0, 0, 0};
     const int64_t steps = (n + 127) / 128;
     // lanes l / 16 = 0..3 hold the 32-column quarters of a step: 16 columns for each of two products
     const int64_t kl = 32 * (lane >> 4);
     int64_t s = wave;
     for (; s + (U - 1) * NW < steps && (s + (U - 1) * NW + 1) * 128 <= n; s += U * NW) {
-        i32x4 a[U][2], b[U][2][TT];
+        i32x4 a[U][2][RT], b[U][2][TT];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t k = (s + u * NW) * 128 + kl + 16 * h;
-                a[u][h] = *reinterpret_cast<const i32x4*>(w + k);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) a[u][h][r] = *reinterpret_cast<const i32x4*>(w[r] + k);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
                     b[u][h][t] = i32x4{0, 0, 0, 0};
@@ -558,28 +563,37 @@ __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __rest
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < TT; ++t)
-                    acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][h], b[u][h][t], acc[t], 0, 0, 0);
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int t = 0; t < TT; ++t)
+                        acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[u][h][r], b[u][h][t], acc[r][t], 0, 0, 0);
     }
     for (; s < steps; s += NW)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int64_t k = s * 128 + kl + 16 * h;
-            const i32x4 a = load(w, k);
+            i32x4 a[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) a[r] = load(w[r], k);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 const i32x4 b = here[t] ? load(x[t], k) : i32x4{0, 0, 0, 0};
-                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc[t], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[r], b, acc[r][t], 0, 0, 0);
             }
         }
     // register e of a 16 x 16 result: row 4 (lane / 16) + e, token lane % 16
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) part[wave][t * 256 + (lane & 15) * 16 + 4 * (lane >> 4) + e] = acc[t][e];
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                part[wave][(16 * t + (lane & 15)) * (16 * RT) + 16 * r + 4 * (lane >> 4) + e] = acc[r][t][e];
     __syncthreads();
-    for (int o = threadIdx.x; o < TT * 256; o += NW * 64) {
-        const int64_t t = o >> 4, i = i0 + (o & 15);
+    for (int o = threadIdx.x; o < TT * RT * 256; o += NW * 64) {
+        const int64_t t = o / (16 * RT), i = i0 + o % (16 * RT);
         if (t >= T || i >= m) continue;
         int32_t v = 0;
 #pragma unroll
@@ -639,13 +653,18 @@ hipError_t tiled(const LinearI8Args& a, hipStream_t st) {
 
 template <class E>
 hipError_t few(const LinearI8Args& a, hipStream_t st) {
-    const dim3 grid((unsigned)((a.m + 15) / 16));
-#define RQ_FEW(TT)                                                                                                    \
-    hipLaunchKernelGGL((linear_i8_few_kernel<TT, E>), grid, dim3(512), 0, st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, \
-                       a.sx, a.sw, a.bias, (E*)a.Y, a.ldy)
-    if (a.T <= 16) RQ_FEW(1);
-    else if (a.T <= 32) RQ_FEW(2);
-    else RQ_FEW(4);
+#define RQ_FEW(TT, RT)                                                                                        \
+    hipLaunchKernelGGL((linear_i8_few_kernel<TT, RT, E>), dim3((unsigned)((a.m + 16 * RT - 1) / (16 * RT))),  \
+                       dim3(512), 0, st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy)
+    // Twice the rows a block halve what its tokens cost, where enough blocks are left (4096 x 14336, 448 blocks:
+    // 16 tokens 18.4 -> 15.5 us; 8192 x 7168, 224 blocks: 64 tokens 40.7 -> 30.5 us, but one token 13.8 -> 19.1 us)
+    const bool tall = a.m >= (a.T > 16 ? 6144 : 12288);
+    if (a.T <= 16 && tall) RQ_FEW(1, 2);
+    else if (a.T <= 16) RQ_FEW(1, 1);
+    else if (a.T <= 32 && tall) RQ_FEW(2, 2);
+    else if (a.T <= 32) RQ_FEW(2, 1);
+    else if (tall) RQ_FEW(4, 2);
+    else RQ_FEW(4, 1);
 #undef RQ_FEW
     return hipGetLastError();
 }

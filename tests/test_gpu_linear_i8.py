@@ -64,7 +64,7 @@ def test_quotients_at_a_half_zeros_tiny_and_bad_rows(rq, ctx, dtype):
 
 
 @pytest.mark.parametrize("T", [1, 2, 5, 16, 17, 33, 64, 65, 128, 300])
-@pytest.mark.parametrize("n,m", [(64, 64), (4096, 512), (1352, 1000), (17, 5), (1, 1), (2000, 77), (14336, 40)])
+@pytest.mark.parametrize("n,m", [(64, 64), (4096, 512), (1352, 1000), (17, 5), (1, 1), (2000, 77), (14336, 40), (80, 12300), (144, 6200)])
 def test_products(rq, ctx, T, n, m):
     print(f"[gpu-case] linear_i8 {T}x{n}x{m}", flush=True)
     g = gen(T * 7 + n)
