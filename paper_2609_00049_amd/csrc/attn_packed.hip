@@ -217,6 +217,21 @@ __device__ __forceinline__ void hold(const uint16_t* __restrict__ g, int hd, int
 
 constexpr int NT = 256, BM = 128;
 
+// f(buffer, i) for i = first, first + step, ... below end, the buffers 0 and 1 in turn and as constants: LDS
+// addresses are then a lane's fixed registers and immediate offsets.
+template <int B>
+struct Buffer {
+    static constexpr int value = B;
+};
+template <class F>
+__device__ __forceinline__ void alternate(int first, int end, int step, F&& f) {
+    for (int i = first; i < end; i += 2 * step) {
+        f(Buffer<0>(), i);
+        if (i + step >= end) break;
+        f(Buffer<1>(), i + step);
+    }
+}
+
 }  // namespace
 
 // The block's head and its rank among the head's tiles, most work first.  Blocks are dealt to the 8 XCDs
@@ -279,7 +294,7 @@ __device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64
 // O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
 // old one serves as well (P up to 256, exact to the same relative rounding).
 template <int HD, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
+__global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
                                                                                        uint16_t* __restrict__ O,
                                                                                        int64_t ldo,
                                                                                        float* __restrict__ lse,
@@ -313,8 +328,8 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_forward_
     f32x16 o[HD / 32];
 #pragma unroll
     for (int t = 0; t < HD / 32; ++t) o[t] = zero16();
-    int buf = 0;
-    for (int k0 = grp * BN; k0 - grp * BN < keys; k0 += GROUPS * BN, buf ^= 1) {
+    alternate(grp * BN, keys + grp * BN, GROUPS * BN, [&](auto buffer, int k0) {
+        constexpr int buf = decltype(buffer)::value;
         vm_wait<0>();
         block_sync();
         const int next = k0 + GROUPS * BN;
@@ -322,7 +337,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_forward_
             loader.load(K, a.ldk, next, sq.len, lds_at(kv_lds[buf ^ 1][0]));
             loader.load(V, a.ldv, next, sq.len, lds_at(kv_lds[buf ^ 1][1]));
         }
-        if (k0 > q0 + 31 || k0 >= keys) continue;  // nothing to see, or a later group's round past the last key
+        if (k0 > q0 + 31 || k0 >= keys) return;  // nothing to see, or a later group's round past the last key
         const uint16_t* sk = kv_lds[buf][0];
         const uint16_t* sv = kv_lds[buf][1];
         f32x16 s[NB];
@@ -372,7 +387,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_forward_
                 for (int t = 0; t < HD / 32; ++t)
                     o[t] = mfma(col_frag<HD>(sv, 32 * b + 16 * x, t, lane), p, o[t]);
             }
-    }
+    });
     l += other_half(l);
     if constexpr (GROUPS == 2) {  // both groups' sums on the larger maximum, through the LDS of the tiles
         float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
@@ -471,8 +486,8 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
     for (int t = 0; t < HD / 32; ++t) g[t] = zero16();
     float sum = 0.f;  // of this lane's part of the row of P dP, then of dS
     auto sweep = [&](bool products) {
-        int buf = 0;
-        for (int k0 = grp * BN; k0 - grp * BN < keys; k0 += GROUPS * BN, buf ^= 1) {
+        alternate(grp * BN, keys + grp * BN, GROUPS * BN, [&](auto buffer, int k0) {
+            constexpr int buf = decltype(buffer)::value;
             vm_wait<0>();
             block_sync();
             const int next = k0 + GROUPS * BN;
@@ -498,10 +513,9 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                     for (int e = 0; e < 16; ++e)
                         if (kb + crow(e, lane) > qi || qi == 0) s[e] = -INFINITY;  // one key: dS is 0
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
-                    sum += s[e];
-                }
+                for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
+                sum += (((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) +
+                       (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));
                 if (!products) continue;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -510,7 +524,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                     for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
                 }
             }
-        }
+        });
     };
     // the sum over both halves of the wave and both groups, in every lane of the query
     auto whole = [&]() {
@@ -636,11 +650,11 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
         fetch(begin + grp, 0, pl, pd);
         keep(0);
     }
-    int buf = 0;
-    for (int i = begin + grp; i - grp < total; i += GROUPS, buf ^= 1) {
+    alternate(begin + grp, total + grp, GROUPS, [&](auto buffer, int i) {
+        constexpr int buf = decltype(buffer)::value;
         vm_wait<0>();
         __syncthreads();
-        if (i >= total) break;  // the last round of the later groups; all waves have passed the same barriers
+        if (i >= total) return;  // the last round of the later groups; all waves have passed the same barriers
         const bool more = i + GROUPS < total;
         if (more) fetch(i + GROUPS, buf ^ 1, pl, pd);
         const int q0 = first + i % steps * BQ;
@@ -696,7 +710,7 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
             __builtin_amdgcn_sched_barrier(0);
         }
         if (more) keep(buf ^ 1);
-    }
+    });
     if constexpr (GROUPS == 2) {  // the second group's sums through the LDS of the tiles, 32 channels at a time
         float* const sum = reinterpret_cast<float*>(qd_lds[0][0][0]) + tid;
         static_assert(sizeof(qd_lds) >= 16 * 256 * 4 && DK && DV, "16 sums a thread");
