@@ -597,7 +597,7 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  * i of a sequence sees its tokens 0 .. i:
  *   O_i = sum_j P_ij v_j,  P_ij = e^(scale q_i k_j - lse_i),  lse_i = log sum_j e^(scale q_i k_j)
  * O: [T, n_heads head_dim] bf16, rows ldo apart; lse: [n_heads, T] float32 | NULL (the backward
- * needs it).  Rows outside every sequence are left as they were.  scale 0 means 1 / sqrt(head_dim).
+ * needs it).  Rows outside every sequence are left as they were, in all outputs.  scale 0 means 1 / sqrt(head_dim).
  * Products of bf16 operands with float32 sums; softmax statistics in float32; the probabilities
  * (and dS in the backward) are rounded to bf16 as operands.
  *
@@ -612,7 +612,7 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  *
  * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
  * 128, 256); every array on 16 bytes and every row stride a multiple of 8, at most 2^24;
- * (T / 128 + n_seqs) n_heads <= 2^23.  q, k, v and dO must be
+ * (T / 128 + n_seqs) n_heads < 2^23.  q, k, v and dO must be
  * finite: a NaN or an infinity can reach every row of its own sequence, and no other sequence.  Offsets that
  * decrease or leave 0 .. T are cut to the arrays, with results of no meaning. */
 typedef struct realq_attention_desc {

@@ -486,7 +486,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
             for (int q = 0; q < LPR / 2; ++q) {
                 const int row = q * (64 / LPR) + lane / LPR;
                 const i32x4 v = *reinterpret_cast<const i32x4*>(own + row * ROW + c);
-                if (tb + row < T) *reinterpret_cast<i32x4*>(Y + (tb + row) * ldy + r0 + c) = v;
+                if (tb + row < T) __builtin_nontemporal_store(v, reinterpret_cast<i32x4*>(Y + (tb + row) * ldy + r0 + c));
             }
         } else {  // an output a lane
             const int rows_here = (int)min(T - tb, (int64_t)32);

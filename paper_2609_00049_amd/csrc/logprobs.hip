@@ -382,7 +382,7 @@ __global__ __launch_bounds__(NT) void backward_kernel(const E* Z, int64_t T, int
     const int tid = threadIdx.x;
     const int n = top + 1;  // the target first, then the alternatives
     for (int64_t item = blockIdx.x; item < T * per_row; item += gridDim.x) {
-        const int64_t t = item / per_row, part = item % per_row;
+        const int64_t t = T - 1 - item / per_row, part = item % per_row;
         const E* z = Z + t * ld;
         E* d = D + t * ldd;
         const int64_t j0 = part * kStretch / (int64_t)sizeof(E);
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(NT) void backward_kernel(const E* Z, int64_t T, int
                         y[e] = __float_as_uint(base(f[e]));
                     }
                 }
-                *reinterpret_cast<u32x4*>(d + a0 + v * N) = y;
+                __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(d + a0 + v * N));
             }
             for (int64_t j = j0 + tid; j < a0; j += NT) d[j] = narrow(base(value(z[j])));
             for (int64_t j = a0 + nv * N + tid; j < j1; j += NT) d[j] = narrow(base(value(z[j])));

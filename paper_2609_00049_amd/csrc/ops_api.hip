@@ -2,7 +2,6 @@
 // probabilities, packed attention and the 8-bit integer product.  Argument checks and launches only; the
 // workspaces are the caller's (a captured graph keeps its own).
 #include <cmath>
-#include <exception>
 #include <string>
 
 #include "common.h"
@@ -42,7 +41,7 @@ int guarded(realq_ctx* ctx, F&& body) {
     if (!ctx) return REALQ_ERR_INVALID_ARG;
     try {
         return body();
-    } catch (const std::exception&) {
+    } catch (...) {
         return REALQ_ERR_OOM;
     }
 }
@@ -74,8 +73,8 @@ int check_attention(realq_ctx* ctx, const realq_attention_desc* d, const char* w
         return set_error(ctx, REALQ_ERR_SHAPE, w + "need 0 <= T <= 2^28, 0 <= n_seqs <= 2^22");
     if (d->n_heads < 1 || d->n_heads > 65535 || d->n_kv < 1 || d->n_heads % d->n_kv)
         return set_error(ctx, REALQ_ERR_SHAPE, w + "need 1 <= n_heads <= 65535, n_kv >= 1 dividing n_heads");
-    if ((d->T / 128 + d->n_seqs) * d->n_heads > (int64_t)1 << 23)
-        return set_error(ctx, REALQ_ERR_SHAPE, w + "need (T / 128 + n_seqs) n_heads <= 2^23");
+    if ((d->T / 128 + d->n_seqs) * d->n_heads >= (int64_t)1 << 23)  // blocks of 512 threads, fewer than 2^32
+        return set_error(ctx, REALQ_ERR_SHAPE, w + "need (T / 128 + n_seqs) n_heads < 2^23");
     if (d->head_dim < 8 || d->head_dim > 256 || d->head_dim % 8)
         return set_error(ctx, REALQ_ERR_SHAPE, w + "head_dim must be a multiple of 8, 8 .. 256");
     if (!(d->scale >= 0.f) || std::isinf(d->scale))

@@ -149,9 +149,11 @@ def attention(L):
     refused(L, -1, "NULL", h, ctypes.byref(desc()), None)
     refused(L, -2, "head_dim", h, ctypes.byref(desc(head_dim=7)), ctypes.byref(n))
     for hd in (8, 64, 128, 256):
-        big = desc(T=(1 << 27) - 128, n_seqs=1, head_dim=hd, ldq=8 * hd, ldk=2 * hd, ldv=2 * hd)
-        assert launched(L, f, *fwd(big, ldo=8 * hd)) >= 1
-        assert launched(L, g, *bwd(big, ldo=8 * hd, lddo=8 * hd, lddq=8 * hd, lddk=2 * hd, lddv=2 * hd)) >= 1
+        for G in (2, 8):
+            big = desc(T=(1 << 27) - 256, n_seqs=1, n_kv=G, head_dim=hd, ldq=8 * hd, ldk=G * hd, ldv=G * hd)
+            assert launched(L, f, *fwd(big, ldo=8 * hd)) >= 1
+            assert launched(L, g, *bwd(big, ldo=8 * hd, lddo=8 * hd, lddq=8 * hd, lddk=G * hd, lddv=G * hd)) >= 1
+    refused(L, -2, "2^23", f, *fwd(desc(T=(1 << 27) - 128, n_seqs=1)))
 
 
 def linear(L):

@@ -111,6 +111,22 @@ def test_largest_sums(rq, ctx, T):
     check(rq, ctx, xq, one[0], wq, one[1], dtype=F32)
 
 
+@pytest.mark.parametrize("T", [3, 70])
+def test_weights_past_32_bits(rq, ctx, T):
+    """Weights and outputs whose last rows lie past 2^31 elements; those rows are checked."""
+    n, m = 65536, 33000
+    g = gen(T)
+    wq = torch.empty((m, n), dtype=I8, device="cuda").random_(-127, 128, generator=g)
+    xq = codes(T, n, g)
+    sx, sw = torch.rand(T, generator=g, device="cuda"), torch.rand(m, generator=g, device="cuda")
+    out = torch.empty((T, 1 << 30), dtype=BF16, device="cuda")[:, :m] if T == 3 else None
+    y = rq.linear_i8(ctx, xq, sx, wq, sw, out=out)
+    want, bound = ref.linear(xq, sx, wq[-100:], sw[-100:])
+    ref.close(y[:, -100:], want, bound + ref.BF * (want.abs() + bound), "last rows")
+    want, bound = ref.linear(xq, sx, wq[:100], sw[:100])
+    ref.close(y[:, :100], want, bound + ref.BF * (want.abs() + bound), "first rows")
+
+
 def test_a_per_row_quantized_module(rq, ctx):
     """The codes, zeros and scales of a module quantized per row (symmetric, the paper's main setting) as integer
     weights: the product is that of the dequantized weights with the dequantized tokens."""

@@ -171,6 +171,24 @@ def test_the_same_bits_again(rq, ctx):
         assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
 
 
+def test_rows_far_apart(rq, ctx):
+    """Rows whose offsets pass 2^31 elements: q, k, v, dO and the gradients in columns of one wide array."""
+    T, H, G, hd, ld = 140, 2, 1, 64, 1 << 24
+    buf = torch.empty(T * ld, dtype=BF16, device="cuda")
+    at = lambda c, n: buf.as_strided((T, n, hd), (ld, hd, 1), c)  # noqa: E731
+    q, k, v, do, cu = make([9, 131], H, G, hd, 13)
+    wide = [at(1024 * i, t.shape[1]) for i, t in enumerate((q, k, v, do))]
+    for w, t in zip(wide, (q, k, v, do)):
+        w.copy_(t)
+    o, lse = check(rq, ctx, *wide, cu)
+    out, grads = at(8192, H), [at(9216 + 1024 * i, n) for i, n in enumerate((H, G, G))]
+    rq.packed_attention(ctx, *wide[:3], cu, out=out)
+    rq.packed_attention_backward(ctx, *wide[:3], cu, out, lse, wide[3], dq=grads[0], dk=grads[1], dv=grads[2])
+    assert torch.equal(out, o)
+    for a, b in zip(grads, rq.packed_attention_backward(ctx, q, k, v, cu, o, lse, do)):
+        assert torch.equal(a, b)
+
+
 def test_offsets_that_lie(rq, ctx):
     """Offsets outside the arrays or in a wrong order are cut to them: no meaning, no access outside, and what
     lies outside every cut sequence stays."""
