@@ -606,8 +606,8 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  *   dV = P^T dO,  dS = P (dO v^T - delta),  delta_i = sum O_i dO_i,  dQ = scale dS k,  dK = scale dS^T q;
  * O and lse as the forward call gave them; work: scratch memory of at least
  * realq_packed_attention_workspace bytes (by T, n_seqs, the heads and head_dim; the arrays are not looked
- * at), aligned to 16, which needs no clearing.  The sums have a fixed order: the same inputs give the same
- * bits.  Outputs must not overlap inputs or each other
+ * at), aligned to 16, which needs no clearing.  The sums have an order fixed by the sizes (T, n_seqs, the heads,
+ * head_dim): the same call gives the same bits.  Outputs must not overlap inputs or each other
  * (rows of one wider array are fine).
  *
  * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
@@ -647,8 +647,8 @@ int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* 
  * realq_linear_i8: Y[t, i] = sx_t sw_i sum_j X[t, j] W[i, j] (+ bias_i), rounded once to dtype from
  * float32.  X: [T, n] int8 rows ldx apart, W: [m, n] int8 rows ldw apart, sx: [T], sw: [m],
  * bias: [m] float32 | NULL, Y: [T, m] rows ldy apart.  The sums are exact (32-bit integers), so
- * n <= REALQ_I8_MAX_COLUMNS.  X and W on 16 bytes with row strides that are multiples of 16 run
- * fastest; others take a path that assembles them byte by byte.  T == 0 is a no-op in both. */
+ * n <= REALQ_I8_MAX_COLUMNS.  For more than 64 tokens X and W on 16 bytes with row strides that are
+ * multiples of 16 run fastest (a third of the time otherwise).  T == 0 is a no-op in both. */
 #define REALQ_I8_MAX_COLUMNS 131071
 int realq_quantize_rows_i8(realq_ctx* ctx, const void* X, int32_t dtype, int64_t T, int64_t n, int64_t ldx, int8_t* Q,
                            int64_t ldq, float* scale);

@@ -776,10 +776,12 @@ namespace {
 bool two_groups(int64_t blocks) { return blocks < 640; }
 // Shares of a dK/dV tile's rounds, for about two blocks a CU: the first keys of a sequence would set the time
 // otherwise (backward of 2048 tokens, 32/8 heads x 128, 136 blocks: 286 us whole, 166 us in 4 shares, 191 us in
-// 8; 2 x 2048, 272 blocks: 342 us whole, 277 us in 2).  544 blocks are faster whole (512 against 560 us).
+// 8; 2 x 2048, 272 blocks: 342 us whole, 277 us in 2).  544 blocks are faster whole (512 against 560 us).  A
+// share has 8 rounds of 32 queries at least if one sequence has all the rows: less does not pay the third launch.
 int key_splits(const AttnArgs& a) {
     const int64_t blocks = (a.T / BM + a.n_seqs) * a.n_kv;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(8, (512 + blocks / 2) / blocks));
+    const int64_t most = std::min<int64_t>(8, a.T * (a.n_heads / a.n_kv) / 256);
+    return (int)std::max<int64_t>(1, std::min(most, (512 + blocks / 2) / blocks));
 }
 
 }  // namespace

@@ -57,6 +57,24 @@ __device__ __forceinline__ void put4(float* p, const float (&y)[4], bool wide, i
     }
 }
 
+// 16- and 8-byte accesses at any address (the target's loads and stores need no alignment)
+struct __attribute__((packed, aligned(1))) Any16 {
+    i32x4 v;
+};
+struct __attribute__((packed, aligned(1))) Any8 {
+    u32x2 v;
+};
+__device__ __forceinline__ i32x4 load16(const void* p) { return reinterpret_cast<const Any16*>(p)->v; }
+// columns k .. k + 15 of a row of n, zeros behind its end
+__device__ __forceinline__ i32x4 load_columns(const int8_t* p, int64_t k, int64_t n) {
+    if (k + 16 <= n) return load16(p + k);
+    i32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[k + e] << (8 * (e & 3)));
+    return v;
+}
+
 constexpr int QT = 256;
 
 }  // namespace
@@ -76,7 +94,7 @@ __device__ __forceinline__ float as_float(E x) {
 
 }  // namespace
 
-// Any strides, alignment and length: two reads of the row, an element a thread.
+// Rows of more than 16384 elements: two reads of the row, an element a thread.
 template <class E>
 __global__ __launch_bounds__(QT) void quantize_any_kernel(const E* __restrict__ X, int64_t T, int64_t n, int64_t ldx,
                                                           int8_t* __restrict__ Q, int64_t ldq,
@@ -98,7 +116,7 @@ __global__ __launch_bounds__(QT) void quantize_any_kernel(const E* __restrict__ 
     }
 }
 
-// Rows on 16 bytes of at most 8 PER threads-per-row elements, held in registers between the maximum and the
+// Rows of at most 8 PER threads-per-row elements, held in registers between the maximum and the
 // codes: one read of X, one write of Q.  RT threads a row (a wave, or a whole block).
 template <class E, int RT, int PER>
 __global__ __launch_bounds__(RT < QT ? QT : RT) void quantize_rows_kernel(const E* __restrict__ X, int64_t T,
@@ -119,11 +137,11 @@ __global__ __launch_bounds__(RT < QT ? QT : RT) void quantize_rows_kernel(const 
             const int64_t j = ((int64_t)p * RT + tid) * 8;
             if (row && j + 8 <= n) {
                 if constexpr (sizeof(E) == 2) {
-                    const u16x8 v = *reinterpret_cast<const u16x8*>(x + j);
+                    const u16x8 v = __builtin_bit_cast(u16x8, load16(x + j));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[p][e] = bf2f(v[e]);
                 } else {
-                    const f32x4 v = *reinterpret_cast<const f32x4*>(x + j), w = *reinterpret_cast<const f32x4*>(x + j + 4);
+                    const f32x4 v = __builtin_bit_cast(f32x4, load16(x + j)), w = __builtin_bit_cast(f32x4, load16(x + j + 4));
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[p][e] = e < 4 ? v[e] : w[e - 4];
                 }
@@ -178,7 +196,7 @@ __global__ __launch_bounds__(RT < QT ? QT : RT) void quantize_rows_kernel(const 
                 v[e] = (uint32_t)(c[4 * e] & 255) | (uint32_t)(c[4 * e + 1] & 255) << 8 |
                        (uint32_t)(c[4 * e + 2] & 255) << 16 | (uint32_t)c[4 * e + 3] << 24;
             if (j + 8 <= n) {
-                *reinterpret_cast<u32x2*>(q + j) = v;
+                reinterpret_cast<Any8*>(q + j)->v = v;
             } else {
                 for (int e = 0; e < 8; ++e)
                     if (j + e < n) q[j + e] = (int8_t)(v[e >> 2] >> (8 * (e & 3)));
@@ -187,7 +205,8 @@ __global__ __launch_bounds__(RT < QT ? QT : RT) void quantize_rows_kernel(const 
     }
 }
 
-// 128 x 128 tile (weights x tokens), 4 waves of 64 x 64, v_mfma_i32_32x32x32_i8; any strides and alignment.
+// 128 x 128 tile (weights x tokens), 4 waves of 64 x 64, v_mfma_i32_32x32x32_i8, staged through registers: prompts
+// with operands that the direct-to-LDS loads do not take (rows not on 16 bytes).
 constexpr int SB = 128, SK = 64, SLD = SK + 16;
 
 template <class E>
@@ -205,18 +224,7 @@ __global__ __launch_bounds__(256) void linear_i8_kernel(const int8_t* __restrict
         for (int b = 0; b < 2; ++b)
             for (int e = 0; e < 16; ++e) acc[a][b][e] = 0;
     auto load = [&](const int8_t* P, int64_t ld, int64_t rows, int64_t r, int64_t k) {
-        i32x4 v = {0, 0, 0, 0};
-        if (r < rows) {
-            const int8_t* p = P + r * ld + k;
-            if (k + 16 <= n && ((uintptr_t)p & 15) == 0) {
-                v = *reinterpret_cast<const i32x4*>(p);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[e] << (8 * (e & 3)));
-            }
-        }
-        return v;
+        return r < rows ? load_columns(P + r * ld, k, n) : i32x4{0, 0, 0, 0};
     };
     for (int64_t k0 = 0; k0 < n; k0 += SK) {
 #pragma unroll
@@ -365,15 +373,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
             const int r = c >> 2;
             const bool w = r < BM;
             const int64_t k = k0 + 16 * (c & 3);
-            const int8_t* p = w ? W + min(i0 + r, m - 1) * ldw + k : X + min(t0 + r - BM, T - 1) * ldx + k;
-            i32x4 v = {0, 0, 0, 0};
-            if (k + 16 <= n) {
-                v = *reinterpret_cast<const i32x4*>(p);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[e] << (8 * (e & 3)));
-            }
+            const int8_t* p = w ? W + min(i0 + r, m - 1) * ldw : X + min(t0 + r - BM, T - 1) * ldx;
+            const i32x4 v = load_columns(p, k, n);
             const int rr = w ? r : r - BM;
             *reinterpret_cast<i32x4*>(stages + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
         }
@@ -523,17 +524,6 @@ __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __rest
         here[t] = 16 * t + (lane & 15) < T;
         x[t] = X + (here[t] ? 16 * t + (lane & 15) : 0) * ldx;
     }
-    auto load = [&](const int8_t* p, int64_t k) {
-        i32x4 v = {0, 0, 0, 0};
-        if (k + 16 <= n) {
-            v = *reinterpret_cast<const i32x4*>(p + k);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[k + e] << (8 * (e & 3)));
-        }
-        return v;
-    };
     i32x4 acc[RT][TT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -551,11 +541,11 @@ __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __rest
             for (int h = 0; h < 2; ++h) {
                 const int64_t k = (s + u * NW) * 128 + kl + 16 * h;
 #pragma unroll
-                for (int r = 0; r < RT; ++r) a[u][h][r] = *reinterpret_cast<const i32x4*>(w[r] + k);
+                for (int r = 0; r < RT; ++r) a[u][h][r] = load16(w[r] + k);
 #pragma unroll
                 for (int t = 0; t < TT; ++t) {
                     b[u][h][t] = i32x4{0, 0, 0, 0};
-                    if (here[t]) b[u][h][t] = *reinterpret_cast<const i32x4*>(x[t] + k);
+                    if (here[t]) b[u][h][t] = load16(x[t] + k);
                 }
             }
 #pragma unroll
@@ -574,10 +564,10 @@ __global__ __launch_bounds__(512) void linear_i8_few_kernel(const int8_t* __rest
             const int64_t k = s * 128 + kl + 16 * h;
             i32x4 a[RT];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) a[r] = load(w[r], k);
+            for (int r = 0; r < RT; ++r) a[r] = load_columns(w[r], k, n);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
-                const i32x4 b = here[t] ? load(x[t], k) : i32x4{0, 0, 0, 0};
+                const i32x4 b = here[t] ? load_columns(x[t], k, n) : i32x4{0, 0, 0, 0};
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
                     acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[r], b, acc[r][t], 0, 0, 0);
@@ -609,12 +599,11 @@ namespace {
 
 template <class E>
 hipError_t quantize(const E* X, int64_t T, int64_t n, int64_t ldx, int8_t* Q, int64_t ldq, float* s, hipStream_t st) {
-    const bool on16 = ((uintptr_t)X & 15) == 0 && ldx * (int64_t)sizeof(E) % 16 == 0 && ((uintptr_t)Q & 7) == 0 && ldq % 8 == 0;
     const unsigned rows = (unsigned)std::min<int64_t>(T, 1 << 20), quads = (unsigned)std::min<int64_t>((T + 3) / 4, 1 << 20);
 #define RQ_ROWS(RT, PER, GRID)                                                                                      \
     hipLaunchKernelGGL((quantize_rows_kernel<E, RT, PER>), dim3(GRID), dim3(RT < QT ? QT : RT), 0, st, X, T, n, ldx, \
                        Q, ldq, s)
-    if (!on16 || n > 16384) hipLaunchKernelGGL(quantize_any_kernel<E>, dim3(rows), dim3(QT), 0, st, X, T, n, ldx, Q, ldq, s);
+    if (n > 16384) hipLaunchKernelGGL(quantize_any_kernel<E>, dim3(rows), dim3(QT), 0, st, X, T, n, ldx, Q, ldq, s);
     else if (n <= 512) RQ_ROWS(64, 1, quads);
     else if (n <= 2048) RQ_ROWS(64, 4, quads);
     else if (n <= 4096) RQ_ROWS(256, 2, rows);
@@ -671,12 +660,14 @@ hipError_t few(const LinearI8Args& a, hipStream_t st) {
 
 template <class E>
 hipError_t linear(const LinearI8Args& a, hipStream_t st) {
-    const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && a.ldx % 16 == 0 && a.ldw % 16 == 0;
-    if (!on16 || a.ldw >= (1 << 22) || a.ldx >= (1 << 22)) return simple<E>(a, st);  // 32-bit offsets in a tile
     // Few tokens: past 16 of them the weights' rows in 64 x 64 tiles, if there are enough for half the CUs
     // (24 tokens, 4096 x 14336: 17 us against 27 us), else the kernel that splits the columns over waves
     // (14336 x 4096: 21 us against 44 us; one token, 4096 x 14336: 15 us against 16 us).
-    if (a.T <= 64 && (a.T <= 16 ? a.m <= 1 << 22 : a.m < 8192)) return few<E>(a, st);
+    const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && (a.T == 1 || a.ldx % 16 == 0) &&
+                      (a.m == 1 || a.ldw % 16 == 0);
+    const bool tiles = on16 && a.ldw < 1 << 22 && a.ldx < 1 << 22;  // 32-bit offsets in a tile
+    if (a.T <= 64 && a.m <= 1 << 22 && (a.T <= 16 || a.m < 8192 || !tiles)) return few<E>(a, st);
+    if (!tiles) return simple<E>(a, st);
     // 256 x 256 tiles where they fill a quarter of the 256 CUs (1024 x 4096 x 4096, 64 tiles: 40 us against 51 us;
     // 2048 x 5120 x 5120: 63 us against 125 us), else 64 x 64 (512 x 4096 x 4096: 20 us against 40 us).
     const int64_t large = ((a.m + 255) / 256) * ((a.T + 255) / 256);
