@@ -267,10 +267,11 @@ __global__ __launch_bounds__(256) void linear_i8_kernel(const int8_t* __restrict
 }
 
 // ---------------------------------------------------------------- prompts: operands on 16 bytes
-// BM weight rows x BN tokens a block, 64 x 128 a wave.  K advances in slices of 64 columns through a ring
-// of three LDS stages filled by direct-to-LDS 16-byte loads: slice s + 2 is in flight while slice s is
-// multiplied.  16-byte chunk c of LDS row r lies at c ^ f(r), so the rows a fragment read touches fall on
-// distinct banks.
+// BM weight rows x BN tokens a block, 32 SM x 32 SN a wave.  K advances in slices of 64 columns through a ring
+// of NS LDS stages filled by direct-to-LDS 16-byte loads: slice s + NS - 1 is in flight while slice s is
+// multiplied.  KG parts of a block, each with waves and a ring of its own, share the columns where blocks are few:
+// one wave a SIMD waits for LDS most of a slice (64 x 64: 0.2 us a slice).  16-byte chunk c of LDS row r lies at
+// c ^ f(r), so the rows a fragment read touches fall on distinct banks.
 namespace {
 
 constexpr int SL = 64;  // columns (bytes) of a slice
@@ -299,19 +300,20 @@ __device__ __forceinline__ void tile_of(int64_t b, int64_t tm, int64_t tn, int64
 
 }  // namespace
 
-template <int WM, int WN, int SM, int SN, int NS, class E>
-__global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
+template <int WM, int WN, int SM, int SN, int NS, int KG, class E>
+__global__ __launch_bounds__(WM* WN* KG * 64, 2) void linear_i8_tile_kernel(
     const int8_t* __restrict__ W, int64_t ldw, const int8_t* __restrict__ X, int64_t ldx, int64_t m, int64_t T,
     int64_t n, const float* __restrict__ sx, const float* __restrict__ sw, const float* __restrict__ bias,
     E* __restrict__ Y, int64_t ldy, int64_t tm, int64_t tn, int64_t band) {
-    constexpr int BM = 32 * SM * WM, BN = 32 * SN * WN, NW = WM * WN, NT = 64 * NW, STAGE = (BM + BN) * SL;
+    constexpr int BM = 32 * SM * WM, BN = 32 * SN * WN, NW = WM * WN, NT = 64 * NW * KG, STAGE = (BM + BN) * SL;
     constexpr int RA = BM / 16 / NW, RB = BN / 16 / NW;  // 1 KB runs (16 rows) a wave loads of each operand
-    __shared__ __attribute__((aligned(16))) int8_t stages[NS * STAGE];
+    __shared__ __attribute__((aligned(16))) int8_t stages[KG * NS * STAGE];
     __shared__ __attribute__((aligned(16))) float rows[2 * BM];  // the tile's output scales and biases
     int64_t ti, tj;
     tile_of(blockIdx.x, tm, tn, band, ti, tj);
     const int64_t i0 = ti * BM, t0 = tj * BN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, at = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = at % NW, part = at / NW;
     const int wm = wave / WN * (32 * SM), wn = wave % WN * (32 * SN);
     i32x16 acc[SM][SN];
 #pragma unroll
@@ -333,9 +335,12 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
         const int r = 16 * (wave + NW * q) + lr;
         ob[q] = (uint32_t)((min(t0 + r, T - 1) - t0) * ldx + 16 * chunk_at(r, lane));
     }
-    const int8_t* const bw = W + i0 * ldw;
-    const int8_t* const bx = X + t0 * ldx;
-    const uint32_t base = lds_at(stages);
+    // a part's run of the whole slices
+    const int64_t full = n / SL, run = (full + KG - 1) / KG, s0 = min(part * run, full), mine = min(run, full - s0);
+    const int8_t* const bw = W + i0 * ldw + s0 * SL;
+    const int8_t* const bx = X + t0 * ldx + s0 * SL;
+    int8_t* const ring = stages + part * (NS * STAGE);
+    const uint32_t base = lds_at(ring);
     auto issue = [&](int64_t s, int st) {
         const uint32_t stage = base + st * STAGE;
 #pragma unroll
@@ -362,7 +367,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
                     acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[i][j], 0, 0, 0);
         }
     };
-    const int64_t full = n / SL;
     for (int r = threadIdx.x; r < BM; r += NT) {
         rows[r] = sw[min(i0 + r, m - 1)];
         rows[BM + r] = bias ? bias[min(i0 + r, m - 1)] : 0.f;
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
             *reinterpret_cast<i32x4*>(stages + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
         }
         __syncthreads();
-        multiply(stages);
+        if (part == 0) multiply(stages);
         __syncthreads();
     }
     if constexpr (NW == 8) {
@@ -437,26 +441,56 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void linear_i8_tile_kernel(
         }
         if (group == 0) __builtin_amdgcn_s_barrier();
     } else {
-        // slice s: its loads have landed, everyone's are visible and nobody reads the stage of slice s - 1 any
-        // more; NS - 1 slices are under way, so a slice waits for memory once in NS - 1
+        // slice s of the part: its loads have landed, everyone's are visible and nobody reads the stage of slice
+        // s - 1 any more; NS - 1 slices are under way, so a slice waits for memory once in NS - 1
         for (int s = 0; s < NS - 1; ++s)
-            if (s < full) issue(s, s);
+            if (s < mine) issue(s, s);
         int st = 0;
-        for (int64_t s = 0; s < full; ++s) {
-            if (s + NS - 2 < full) vm_wait<(NS - 2) * (RA + RB)>();
+        for (int64_t s = 0; s < run; ++s) {
+            if (s + NS - 2 < mine) vm_wait<(NS - 2) * (RA + RB)>();
             else vm_wait<0>();
             __builtin_amdgcn_s_barrier();
             const int before = st == 0 ? NS - 1 : st - 1;
-            if (s + NS - 1 < full) issue(s + NS - 1, before);
-            multiply(stages + st * STAGE);
+            if (s + NS - 1 < mine) issue(s + NS - 1, before);
+            if (KG == 1 || s < mine) multiply(ring + st * STAGE);
             st = st + 1 == NS ? 0 : st + 1;
         }
+    }
+    __syncthreads();
+    if constexpr (KG > 1) {  // the parts' sums, in the rings behind the first
+        constexpr int SUMS = SM * SN * 4;
+        static_assert(NW * 64 * SUMS * 16 <= NS * STAGE, "a ring holds the sums");
+        i32x4* const sums = reinterpret_cast<i32x4*>(stages) + wave * SUMS * 64 + lane;
+        if (part > 0) {
+            i32x4* const to = sums + part * (NS * STAGE / 16);
+#pragma unroll
+            for (int i = 0; i < SM; ++i)
+#pragma unroll
+                for (int j = 0; j < SN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        to[((i * SN + j) * 4 + e) * 64] =
+                            i32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]};
+        }
+        __syncthreads();
+        if (part > 0) return;
+#pragma unroll
+        for (int g = 1; g < KG; ++g)
+#pragma unroll
+            for (int i = 0; i < SM; ++i)
+#pragma unroll
+                for (int j = 0; j < SN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const i32x4 v = sums[g * (NS * STAGE / 16) + ((i * SN + j) * 4 + e) * 64];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) acc[i][j][4 * e + x] += v[x];
+                    }
     }
     // The wave's 32 SM outputs of 32 tokens at a time, through LDS of its own so that the stores are whole lines:
     // a lane holds one token and 4 consecutive outputs, and stores 16 bytes of a token's outputs.
     constexpr int OUT = 32 * SM, PER = 16 / (int)sizeof(E), LPR = OUT / PER, ROW = OUT + PER;  // lanes a token, LDS row
     static_assert(NW * 32 * ROW * (int)sizeof(E) <= NS * STAGE, "the stages hold the outputs");
-    __syncthreads();
     E* const own = reinterpret_cast<E*>(stages) + wave * (32 * ROW);
     const bool wide = ldy % PER == 0 && ((uintptr_t)Y & 15) == 0;
     const int64_t r0 = i0 + wm;
@@ -631,11 +665,11 @@ hipError_t simple(const LinearI8Args& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int WM, int WN, int SM, int SN, int NS, class E>
+template <int WM, int WN, int SM, int SN, int NS, int KG, class E>
 hipError_t tiled(const LinearI8Args& a, hipStream_t st) {
     constexpr int BM = 32 * SM * WM, BN = 32 * SN * WN;
     const int64_t tm = (a.m + BM - 1) / BM, tn = (a.T + BN - 1) / BN;
-    hipLaunchKernelGGL((linear_i8_tile_kernel<WM, WN, SM, SN, NS, E>), dim3((unsigned)(tm * tn)), dim3(WM * WN * 64), 0,
+    hipLaunchKernelGGL((linear_i8_tile_kernel<WM, WN, SM, SN, NS, KG, E>), dim3((unsigned)(tm * tn)), dim3(WM * WN * KG * 64), 0,
                        st, a.W, a.ldw, a.X, a.ldx, a.m, a.T, a.n, a.sx, a.sw, a.bias, (E*)a.Y, a.ldy, tm, tn, 8);
     return hipGetLastError();
 }
@@ -660,19 +694,22 @@ hipError_t few(const LinearI8Args& a, hipStream_t st) {
 
 template <class E>
 hipError_t linear(const LinearI8Args& a, hipStream_t st) {
-    // Few tokens: past 16 of them the weights' rows in 64 x 64 tiles, if there are enough for half the CUs
-    // (24 tokens, 4096 x 14336: 17 us against 27 us), else the kernel that splits the columns over waves
-    // (14336 x 4096: 21 us against 44 us; one token, 4096 x 14336: 15 us against 16 us).
     const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && (a.T == 1 || a.ldx % 16 == 0) &&
                       (a.m == 1 || a.ldw % 16 == 0);
     const bool tiles = on16 && a.ldw < 1 << 22 && a.ldx < 1 << 22;  // 32-bit offsets in a tile
-    if (a.T <= 64 && a.m <= 1 << 22 && (a.T <= 16 || a.m < 8192 || !tiles)) return few<E>(a, st);
+    // Up to 32 tokens the kernel that splits the columns over waves, as long as the tiles' blocks are few as well
+    // (24 tokens, 14336 x 4096: 20 us against 28 us; but 32 tokens, 8192 x 8192: 23 us against 20 us).
+    if (a.T <= 64 && a.m <= 1 << 22 && (a.T <= 16 || (a.T <= 32 && a.m < 6144) || !tiles)) return few<E>(a, st);
     if (!tiles) return simple<E>(a, st);
-    // 256 x 256 tiles where they fill a quarter of the 256 CUs (1024 x 4096 x 4096, 64 tiles: 40 us against 51 us;
-    // 2048 x 5120 x 5120: 63 us against 125 us), else 64 x 64 (512 x 4096 x 4096: 20 us against 40 us).
-    const int64_t large = ((a.m + 255) / 256) * ((a.T + 255) / 256);
-    if (large < 64) return tiled<2, 2, 1, 1, 6, E>(a, st);
-    return tiled<4, 2, 2, 4, 3, E>(a, st);
+    auto blocks = [&](int64_t side) { return ((a.m + side - 1) / side) * ((a.T + side - 1) / side); };
+    // 64 x 64 tiles: one to each of the 256 CUs or less, and four parts of the columns share it (256 x 3000 x 4000:
+    // 12.5 us against 15.3 us with one; 96 x 14336 x 4096: 31 us against 44 us); up to three fit a CU.  Past that
+    // 128 x 128 (1024 x 4096 x 4096: 27 us against 40 us), until 256 x 256 fill almost half of the CUs (1800 x 2048
+    // x 5120, 160 tiles: 27 us against 34 us; 1536 x 4096 x 4096, 96 tiles: 40 us against 37 us).
+    if (blocks(64) <= 256) return tiled<2, 2, 1, 1, 4, 4, E>(a, st);
+    if (blocks(64) < 768) return tiled<2, 2, 1, 1, 6, 1, E>(a, st);
+    if (blocks(256) < 112) return tiled<2, 2, 2, 2, 3, 1, E>(a, st);
+    return tiled<4, 2, 2, 4, 3, 1, E>(a, st);
 }
 
 }  // namespace
