@@ -697,18 +697,25 @@ hipError_t linear(const LinearI8Args& a, hipStream_t st) {
     const bool on16 = (((uintptr_t)a.X | (uintptr_t)a.W) & 15) == 0 && (a.T == 1 || a.ldx % 16 == 0) &&
                       (a.m == 1 || a.ldw % 16 == 0);
     const bool tiles = on16 && a.ldw < 1 << 22 && a.ldx < 1 << 22;  // 32-bit offsets in a tile
-    // Up to 32 tokens the kernel that splits the columns over waves, as long as the tiles' blocks are few as well
-    // (24 tokens, 14336 x 4096: 20 us against 28 us; but 32 tokens, 8192 x 8192: 23 us against 20 us).
-    if (a.T <= 64 && a.m <= 1 << 22 && (a.T <= 16 || (a.T <= 32 && a.m < 6144) || !tiles)) return few<E>(a, st);
+    // Up to 16 tokens the kernel that splits the columns over waves (16 tokens, 14336 x 4096: 16 us against 18 us;
+    // 24 tokens: 20 us against 18 us).
+    if (a.T <= 64 && a.m <= 1 << 22 && (a.T <= 16 || !tiles)) return few<E>(a, st);
     if (!tiles) return simple<E>(a, st);
-    auto blocks = [&](int64_t side) { return ((a.m + side - 1) / side) * ((a.T + side - 1) / side); };
-    // 64 x 64 tiles: one to each of the 256 CUs or less, and four parts of the columns share it (256 x 3000 x 4000:
-    // 12.5 us against 15.3 us with one; 96 x 14336 x 4096: 31 us against 44 us); up to three fit a CU.  Past that
-    // 128 x 128 (1024 x 4096 x 4096: 27 us against 40 us), until 256 x 256 fill almost half of the CUs (1800 x 2048
-    // x 5120, 160 tiles: 27 us against 34 us; 1536 x 4096 x 4096, 96 tiles: 40 us against 37 us).
-    if (blocks(64) <= 256) return tiled<2, 2, 1, 1, 4, 4, E>(a, st);
-    if (blocks(64) < 768) return tiled<2, 2, 1, 1, 6, 1, E>(a, st);
-    if (blocks(256) < 112) return tiled<2, 2, 2, 2, 3, 1, E>(a, st);
+    auto blocks = [&](int64_t rows, int64_t tokens) {
+        return ((a.m + rows - 1) / rows) * ((a.T + tokens - 1) / tokens);
+    };
+    // The smallest tile of which every one of the 256 CUs gets at most one: what a block waits for in its loads sets
+    // the time, so the more CUs load the better (with the quantizer before: 81 tokens, 11492 x 877: 32 x 32 30 us,
+    // 64 x 64 44 us; 96 tokens, 14336 x 4096: 64 x 32 34 us, 32 x 32 45 us, 64 x 64 38 us, all of whose columns one
+    // part takes 53 us; 256 tokens, 14336 x 4096: 64 x 64 46 us, 64 x 32 64 us).  Past that 64 x 64 in one part, up
+    // to three on a CU, then 128 x 128 (1024 x 4096 x 4096: 27 us against 40 us), until 256 x 256 fill almost half
+    // of the CUs (1800 x 2048 x 5120, 160 tiles: 27 us against 34 us; 1536 x 4096 x 4096, 96 tiles: 40 us against
+    // 37 us).
+    if (blocks(32, 32) <= 256) return tiled<1, 1, 1, 1, 4, 8, E>(a, st);
+    if (blocks(64, 32) <= 256) return tiled<2, 1, 1, 1, 4, 4, E>(a, st);
+    if (blocks(64, 64) <= 256) return tiled<2, 2, 1, 1, 4, 4, E>(a, st);
+    if (blocks(64, 64) < 768) return tiled<2, 2, 1, 1, 6, 1, E>(a, st);
+    if (blocks(256, 256) < 112) return tiled<2, 2, 2, 2, 3, 1, E>(a, st);
     return tiled<4, 2, 2, 4, 3, 1, E>(a, st);
 }
 

@@ -86,10 +86,10 @@ def test_large_products(rq, ctx, T, n, m):
     check(rq, ctx, xq, sx, wq, sw, None, F32)
 
 
-@pytest.mark.parametrize("T,m", [(66, 1000), (520, 5500), (3700, 2050)], ids=["few", "some", "many"])
+@pytest.mark.parametrize("T,m", [(66, 1000), (90, 4000), (250, 3900), (300, 4000), (520, 5500), (3700, 2050)])
 @pytest.mark.parametrize("n", [1, 50, 64, 127, 128, 200, 450, 1090])
 def test_numbers_of_tiles_and_slices(rq, ctx, T, m, n):
-    """A few, some and many tiles of outputs, over columns of less than a slice, one to seventeen and a rest."""
+    """From a few tiles of outputs to many, over columns of less than a slice, one to seventeen and a rest."""
     g = gen(n + m)
     xq, wq = codes(T, n, g, -n % 16), codes(m, n, g, -n % 16)
     sx, sw = torch.rand(T, generator=g, device="cuda"), torch.rand(m, generator=g, device="cuda")
