@@ -610,7 +610,7 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  * head_dim): the same call gives the same bits.  Outputs must not overlap inputs or each other
  * (rows of one wider array are fine).
  *
- * head_dim a multiple of 8, at most 256 (64 and 128 run fastest; others compute on the next of 64,
+ * head_dim a multiple of 8, at most 256 (64, 96 and 128 run fastest; others compute on the next of 64, 96,
  * 128, 256); every array on 16 bytes and every row stride a multiple of 8, at most 2^24;
  * (T / 128 + n_seqs) n_heads < 2^23.  q, k, v and dO must be
  * finite: a NaN or an infinity can reach every row of its own sequence, and no other sequence.  Offsets that

@@ -194,10 +194,10 @@ struct Loader {
         }
     }
 };
-// Zeros in the channels from hd on of a tile.
-template <int HD, int ROWS, int NT>
+// Zeros in the channels from hd on of a tile, where the kernel computes on them.
+template <int HD, int HC, int ROWS, int NT>
 __device__ __forceinline__ void clear_rest(uint16_t* lds, int hd) {
-    if (hd == HD) return;
+    if (hd == HC) return;
     for (int i = threadIdx.x; i < ROWS * HD / 8; i += NT)
         *reinterpret_cast<u16x8*>(lds + i * 8) = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
     __syncthreads();
@@ -293,7 +293,7 @@ __device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64
 // maximum, sum and rescaling are the lane's own; only the maximum and the final sum cross to lane + 32.
 // O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
 // old one serves as well (P up to 256, exact to the same relative rounding).
-template <int HD, int GROUPS>
+template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
                                                                                        uint16_t* __restrict__ O,
                                                                                        int64_t ldo,
@@ -314,20 +314,20 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
     const int qi = min(q0 + (lane & 31), sq.len - 1);  // this lane's
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
-    clear_rest<HD, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
+    clear_rest<HD, HC, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
     const Loader<HD, BN, 4> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
     if (grp * BN < keys) {
         loader.load(K, a.ldk, grp * BN, sq.len, lds_at(kv_lds[0][0]));
         loader.load(V, a.ldv, grp * BN, sq.len, lds_at(kv_lds[0][1]));
     }
-    bf16x8 qf[HD / 16];
-    hold<HD>(a.q + (sq.begin + qi) * a.ldq + h * a.hd, a.hd, lane, qf);
+    bf16x8 qf[HC / 16];
+    hold<HC>(a.q + (sq.begin + qi) * a.ldq + h * a.hd, a.hd, lane, qf);
     const float c = a.scale * kLog2e;
     float m = -INFINITY, mc = 0.f, l = 0.f;
-    f32x16 o[HD / 32];
+    f32x16 o[HC / 32];
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t) o[t] = zero16();
+    for (int t = 0; t < HC / 32; ++t) o[t] = zero16();
     alternate(grp * BN, keys + grp * BN, GROUPS * BN, [&](auto buffer, int k0) {
         constexpr int buf = decltype(buffer)::value;
         vm_wait<0>();
@@ -344,10 +344,10 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
 #pragma unroll
         for (int b = 0; b < NB; ++b) s[b] = zero16();
 #pragma unroll
-        for (int u = 0; u < HD / 16; ++u)
+        for (int u = 0; u < HC / 16; ++u)
 #pragma unroll
             for (int b = 0; b < NB; ++b) s[b] = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s[b]);
-        order_reads<HD / 16 * NB, HD / 16 * NB, AHEAD>();
+        order_reads<HC / 16 * NB, HC / 16 * NB, AHEAD>();
         if (k0 + BN - 1 > q0)  // a tile that some query of the wave sees in part
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
             mc = m * c;
             l *= f;
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t)
+            for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[t][e] *= f;
         }
@@ -384,20 +384,20 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
             for (int x = 0; x < 2; ++x) {
                 const bf16x8 p = pack_frag(s[b], x);
 #pragma unroll
-                for (int t = 0; t < HD / 32; ++t)
+                for (int t = 0; t < HC / 32; ++t)
                     o[t] = mfma(col_frag<HD>(sv, 32 * b + 16 * x, t, lane), p, o[t]);
             }
     });
     l += other_half(l);
     if constexpr (GROUPS == 2) {  // both groups' sums on the larger maximum, through the LDS of the tiles
         float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
-        static_assert(sizeof(all_lds) >= (HD / 2 + 2) * 256 * 4, "a thread's sums");
+        static_assert(sizeof(all_lds) >= (HC / 2 + 2) * 256 * 4, "a thread's sums");
         __syncthreads();
         if (grp == 1) {
             sh[0] = m;
             sh[256] = l;
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t)
+            for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sh[(2 + 16 * t + e) * 256] = o[t][e];
         }
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
         m = mn;
         l = l * f0 + sh[256] * f1;
 #pragma unroll
-        for (int t = 0; t < HD / 32; ++t)
+        for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[t][e] = o[t][e] * f0 + sh[(2 + 16 * t + e) * 256] * f1;
     }
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
     const float inv = 1.f / l;
     uint16_t* out = O + row * ldo + h * a.hd;
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t)
+    for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int ch = 32 * t + crow(e, lane);
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
 // has one large entry.  What it is off by is the sum of a row of dS (which is 0 for the true delta): that sum
 // goes into the delta stored for dK, and for the first tile of a sequence, whose rows see few keys (2 keys:
 // 6e-3 of dQ; 300: 2e-3), a pass over its keys forms delta as sum P dP first.
-template <int HD, int GROUPS>
+template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
     const uint16_t* __restrict__ dO, int64_t lddo, float* __restrict__ delta, uint16_t* __restrict__ dQ, int64_t lddq,
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
     const int64_t row = sq.begin + qi;
     const uint16_t* K = a.k + sq.begin * a.ldk + kv * a.hd;
     const uint16_t* V = a.v + sq.begin * a.ldv + kv * a.hd;
-    clear_rest<HD, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
+    clear_rest<HD, HC, GROUPS * 4 * BN, 256 * GROUPS>(all_lds[0][0][0], a.hd);
     const Loader<HD, BN, 4> loader(a.hd, wave);
     const int keys = min((sq.tile + 1) * BM, sq.len);
     auto begin = [&]() {
@@ -466,24 +466,24 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
         }
     };
     begin();
-    bf16x8 qf[HD / 16], df[HD / 16];
-    hold<HD>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
-    hold<HD>(dO + row * lddo + h * a.hd, a.hd, lane, df);
+    bf16x8 qf[HC / 16], df[HC / 16];
+    hold<HC>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
+    hold<HC>(dO + row * lddo + h * a.hd, a.hd, lane, df);
     float dl = 0.f;
     {
-        bf16x8 of[HD / 16];
-        hold<HD>(O + row * ldo + h * a.hd, a.hd, lane, of);
+        bf16x8 of[HC / 16];
+        hold<HC>(O + row * ldo + h * a.hd, a.hd, lane, of);
 #pragma unroll
-        for (int s = 0; s < HD / 16; ++s)
+        for (int s = 0; s < HC / 16; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) dl += (float)of[s][e] * (float)df[s][e];
         dl += other_half(dl);
     }
     const bool live = q0 + (lane & 31) < sq.len;
     const float c = a.scale * kLog2e, L = lse[(int64_t)h * a.T + row] * kLog2e;
-    f32x16 g[HD / 32];
+    f32x16 g[HC / 32];
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t) g[t] = zero16();
+    for (int t = 0; t < HC / 32; ++t) g[t] = zero16();
     float sum = 0.f;  // of this lane's part of the row of P dP, then of dS
     auto sweep = [&](bool products) {
         alternate(grp * BN, keys + grp * BN, GROUPS * BN, [&](auto buffer, int k0) {
@@ -503,11 +503,11 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                 if (kb > q0 + 31 || kb >= keys) continue;
                 f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-                for (int u = 0; u < HD / 16; ++u) {
+                for (int u = 0; u < HC / 16; ++u) {
                     s = mfma(row_frag<HD>(sk, 32 * b, u, lane), qf[u], s);
                     dp = mfma(row_frag<HD>(sv, 32 * b, u, lane), df[u], dp);
                 }
-                order_reads<HD / 8, HD / 8, AHEAD>();
+                order_reads<HC / 8, HC / 8, AHEAD>();
                 if (kb + 31 > q0)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                 for (int x = 0; x < 2; ++x) {
                     const bf16x8 d = pack_frag(s, x);
 #pragma unroll
-                    for (int t = 0; t < HD / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
+                    for (int t = 0; t < HC / 32; ++t) g[t] = mfma(col_frag<HD>(sk, 32 * b + 16 * x, t, lane), d, g[t]);
                 }
             }
         });
@@ -549,24 +549,24 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
     if (live && grp == 0 && lane < 32) delta[(int64_t)h * a.T + row] = dl + off;
     if constexpr (GROUPS == 2) {
         float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
-        static_assert(sizeof(all_lds) >= HD / 2 * 256 * 4, "a thread's sums");
+        static_assert(sizeof(all_lds) >= HC / 2 * 256 * 4, "a thread's sums");
         __syncthreads();
         if (grp == 1)
 #pragma unroll
-            for (int t = 0; t < HD / 32; ++t)
+            for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) sh[(16 * t + e) * 256] = g[t][e];
         __syncthreads();
         if (grp == 1) return;
 #pragma unroll
-        for (int t = 0; t < HD / 32; ++t)
+        for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) g[t][e] += sh[(16 * t + e) * 256];
     }
     if (!live) return;
     uint16_t* out = dQ + row * lddq + h * a.hd;
 #pragma unroll
-    for (int t = 0; t < HD / 32; ++t)
+    for (int t = 0; t < HC / 32; ++t)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             const int ch = 32 * t + crow(e, lane);
@@ -586,12 +586,12 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
 // their 256 registers; DK, DV: what this launch forms (both, or one each where both do not fit).  With splits > 1
 // a block takes one of that many shares of its tile's rounds and leaves float32 sums in `part`
 // ([split][dK, dV][T][n_kv hd]), which sum_splits_kernel adds in their order.
-template <int HD, int GROUPS, bool KL, bool DK, bool DV>
+template <int HD, int HC, int GROUPS, bool KL, bool DK, bool DV>
 __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
     const float* __restrict__ delta, uint16_t* __restrict__ dK, int64_t lddk, uint16_t* __restrict__ dV, int64_t lddv,
     int64_t tiles, int splits, float* __restrict__ part) {
-    constexpr int BQ = 32, THREADS = 256 * GROUPS, ACC = HD / 32;
+    constexpr int BQ = 32, THREADS = 256 * GROUPS, ACC = HC / 32;
     __shared__ __attribute__((aligned(16))) uint16_t qd_lds[GROUPS][2][2][BQ * HD];
     __shared__ __attribute__((aligned(16))) uint16_t kv_lds[2][KL ? BM * HD : 8];
     __shared__ __attribute__((aligned(16))) float stat[GROUPS][2][2][BQ];  // lse in units of log 2, delta
@@ -608,17 +608,17 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = all >> 2, wave = all & 3;
     const int k0 = sq.tile * BM + wave * 32;
     const int ki = min(k0 + (lane & 31), sq.len - 1);
-    clear_rest<HD, GROUPS * 4 * BQ, THREADS>(qd_lds[0][0][0], a.hd);
+    clear_rest<HD, HC, GROUPS * 4 * BQ, THREADS>(qd_lds[0][0][0], a.hd);
     if constexpr (KL) {
-        clear_rest<HD, 2 * BM, THREADS>(kv_lds[0], a.hd);
+        clear_rest<HD, HC, 2 * BM, THREADS>(kv_lds[0], a.hd);
         const Loader<HD, BM, 4 * GROUPS> keys(a.hd, all);
         keys.load(a.k + sq.begin * a.ldk + kv * a.hd, a.ldk, sq.tile * BM, sq.len, lds_at(kv_lds[0]));
         keys.load(a.v + sq.begin * a.ldv + kv * a.hd, a.ldv, sq.tile * BM, sq.len, lds_at(kv_lds[1]));
     }
     const Loader<HD, BQ, 4> loader(a.hd, wave);
-    bf16x8 kf[KL ? 1 : HD / 16], vf[DK && !KL ? HD / 16 : 1];
-    if constexpr (!KL) hold<HD>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
-    if constexpr (DK && !KL) hold<HD>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
+    bf16x8 kf[KL ? 1 : HC / 16], vf[DK && !KL ? HC / 16 : 1];
+    if constexpr (!KL) hold<HC>(a.k + (sq.begin + ki) * a.ldk + kv * a.hd, a.hd, lane, kf);
+    if constexpr (DK && !KL) hold<HC>(a.v + (sq.begin + ki) * a.ldv + kv * a.hd, a.hd, lane, vf);
     const float c = a.scale * kLog2e;
     f32x16 gk[DK ? ACC : 1], gv[DV ? ACC : 1];
 #pragma unroll
@@ -666,7 +666,7 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
             if (qb + 31 < k0) continue;
             f32x16 s = zero16(), dp = zero16();
 #pragma unroll
-            for (int u = 0; u < HD / 16; ++u) {
+            for (int u = 0; u < HC / 16; ++u) {
                 bf16x8 k, v;
                 if constexpr (KL) {
                     k = row_frag<HD>(kv_lds[0], wave * 32, u, lane);
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
                 s = mfma(row_frag<HD>(sqr, 32 * b, u, lane), k, s);
                 if constexpr (DK) dp = mfma(row_frag<HD>(sdo, 32 * b, u, lane), v, dp);
             }
-            order_reads<HD / 16 * (1 + KL) * (1 + DK), HD / 16 * (1 + DK), KL ? 8 : 6>();
+            order_reads<HC / 16 * (1 + KL) * (1 + DK), HC / 16 * (1 + DK), KL ? 8 : 6>();
             if (qb < k0 + 31 || qb + 32 > sq.len)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -789,11 +789,14 @@ int key_splits(const AttnArgs& a) {
 #define RQ_HEAD_DIM(KERNEL, BLOCKS, ...)                                                                              \
     do {                                                                                                              \
         const dim3 g_((unsigned)(BLOCKS));                                                                            \
-        if (a.hd > 128) hipLaunchKernelGGL((KERNEL<256, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                      \
-        else if (two_groups(BLOCKS) && a.hd <= 64) hipLaunchKernelGGL((KERNEL<64, 2>), g_, dim3(512), 0, st, __VA_ARGS__);   \
-        else if (two_groups(BLOCKS)) hipLaunchKernelGGL((KERNEL<128, 2>), g_, dim3(512), 0, st, __VA_ARGS__);         \
-        else if (a.hd <= 64) hipLaunchKernelGGL((KERNEL<64, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                  \
-        else hipLaunchKernelGGL((KERNEL<128, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                                 \
+        const bool two = two_groups(BLOCKS);                                                                          \
+        if (a.hd > 128) hipLaunchKernelGGL((KERNEL<256, 256, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                 \
+        else if (a.hd > 96 && two) hipLaunchKernelGGL((KERNEL<128, 128, 2>), g_, dim3(512), 0, st, __VA_ARGS__);      \
+        else if (a.hd > 96) hipLaunchKernelGGL((KERNEL<128, 128, 1>), g_, dim3(256), 0, st, __VA_ARGS__);             \
+        else if (a.hd > 64 && two) hipLaunchKernelGGL((KERNEL<128, 96, 2>), g_, dim3(512), 0, st, __VA_ARGS__);       \
+        else if (a.hd > 64) hipLaunchKernelGGL((KERNEL<128, 96, 1>), g_, dim3(256), 0, st, __VA_ARGS__);              \
+        else if (two) hipLaunchKernelGGL((KERNEL<64, 64, 2>), g_, dim3(512), 0, st, __VA_ARGS__);                     \
+        else hipLaunchKernelGGL((KERNEL<64, 64, 1>), g_, dim3(256), 0, st, __VA_ARGS__);                              \
     } while (0)
 
 hipError_t attn_packed_forward(const AttnArgs& a, uint16_t* O, int64_t ldo, float* lse, hipStream_t st) {
@@ -818,16 +821,18 @@ hipError_t attn_packed_backward(const AttnArgs& a, const uint16_t* O, int64_t ld
     const int splits = key_splits(a);
     float* const part = delta + (a.n_heads * a.T + 3) / 4 * 4;
     const dim3 grid((unsigned)(tiles * a.n_kv * splits));
-#define RQ_DKV(HD, GROUPS, KL, DK, DV)                                                                               \
-    hipLaunchKernelGGL((attn_dkv_kernel<HD, GROUPS, KL, DK, DV>), grid, dim3(256 * GROUPS), 0, st, a, lse, dO, lddo, \
-                       delta, dK, lddk, dV, lddv, tiles, splits, part)
+#define RQ_DKV(HD, HC, GROUPS, KL, DK, DV)                                                                           \
+    hipLaunchKernelGGL((attn_dkv_kernel<HD, HC, GROUPS, KL, DK, DV>), grid, dim3(256 * GROUPS), 0, st, a, lse, dO,   \
+                       lddo, delta, dK, lddk, dV, lddv, tiles, splits, part)
     if (a.hd <= 64) {
-        RQ_DKV(64, 2, false, true, true);
+        RQ_DKV(64, 64, 2, false, true, true);
+    } else if (a.hd <= 96) {
+        RQ_DKV(128, 96, 2, true, true, true);
     } else if (a.hd <= 128) {
-        RQ_DKV(128, 2, true, true, true);
+        RQ_DKV(128, 128, 2, true, true, true);
     } else {
-        RQ_DKV(256, 1, false, false, true);
-        RQ_DKV(256, 1, false, true, false);
+        RQ_DKV(256, 256, 1, false, false, true);
+        RQ_DKV(256, 256, 1, false, true, false);
     }
 #undef RQ_DKV
     if (splits > 1) {

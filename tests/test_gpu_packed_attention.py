@@ -48,6 +48,12 @@ def test_heads(rq, ctx, H, G, hd):
     check(rq, ctx, *make([40, 150, 1], H, G, hd, 1))
 
 
+@pytest.mark.parametrize("hd", [64, 88, 96, 104, 128])
+@pytest.mark.parametrize("lens", [[900], [900] + [5] * 150], ids=["few", "many"])
+def test_head_sizes_in_few_and_many_tiles(rq, ctx, lens, hd):
+    check(rq, ctx, *make(lens, 4, 1, hd, 5))
+
+
 @pytest.mark.parametrize("scale", [0.01, 0.5])
 def test_scales_and_wide_scores(rq, ctx, scale):
     """Flat and saturated softmaxes."""
