@@ -94,7 +94,7 @@ __device__ __forceinline__ float as_float(E x) {
 
 }  // namespace
 
-// Rows of more than 16384 elements: two reads of the row, an element a thread.
+// Rows of more than 32768 elements: two reads of the row, an element a thread.
 template <class E>
 __global__ __launch_bounds__(QT) void quantize_any_kernel(const E* __restrict__ X, int64_t T, int64_t n, int64_t ldx,
                                                           int8_t* __restrict__ Q, int64_t ldq,
@@ -637,12 +637,13 @@ hipError_t quantize(const E* X, int64_t T, int64_t n, int64_t ldx, int8_t* Q, in
 #define RQ_ROWS(RT, PER, GRID)                                                                                      \
     hipLaunchKernelGGL((quantize_rows_kernel<E, RT, PER>), dim3(GRID), dim3(RT < QT ? QT : RT), 0, st, X, T, n, ldx, \
                        Q, ldq, s)
-    if (n > 16384) hipLaunchKernelGGL(quantize_any_kernel<E>, dim3(rows), dim3(QT), 0, st, X, T, n, ldx, Q, ldq, s);
+    if (n > 32768) hipLaunchKernelGGL(quantize_any_kernel<E>, dim3(rows), dim3(QT), 0, st, X, T, n, ldx, Q, ldq, s);
     else if (n <= 512) RQ_ROWS(64, 1, quads);
     else if (n <= 2048) RQ_ROWS(64, 4, quads);
     else if (n <= 4096) RQ_ROWS(256, 2, rows);
     else if (n <= 8192) RQ_ROWS(256, 4, rows);
-    else RQ_ROWS(512, 4, rows);
+    else if (n <= 16384) RQ_ROWS(512, 4, rows);
+    else RQ_ROWS(1024, 4, rows);
 #undef RQ_ROWS
     return hipGetLastError();
 }

@@ -29,7 +29,7 @@ def check(rq, ctx, xq, sx, wq, sw, bias=None, dtype=BF16, out=None):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
-@pytest.mark.parametrize("T,n", [(1, 1), (1, 4096), (3, 15), (7, 1352), (2, 14336), (130, 257), (5, 33001), (9, 16)])
+@pytest.mark.parametrize("T,n", [(1, 1), (1, 4096), (3, 15), (7, 1352), (2, 14336), (130, 257), (5, 33001), (9, 16), (3, 20001), (2, 32768)])
 def test_codes_and_scales_are_those_of_exact_quotients(rq, ctx, T, n, dtype):
     x = (torch.randn((T, n), generator=gen(n), device="cuda") * torch.exp(torch.randn(n, generator=gen(1), device="cuda"))).to(dtype)
     q, s = rq.quantize_rows_i8(ctx, x)
