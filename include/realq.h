@@ -647,8 +647,9 @@ int realq_packed_attention_backward(realq_ctx* ctx, const realq_attention_desc* 
  * realq_linear_i8: Y[t, i] = sx_t sw_i sum_j X[t, j] W[i, j] (+ bias_i), rounded once to dtype from
  * float32.  X: [T, n] int8 rows ldx apart, W: [m, n] int8 rows ldw apart, sx: [T], sw: [m],
  * bias: [m] float32 | NULL, Y: [T, m] rows ldy apart.  The sums are exact (32-bit integers), so
- * n <= REALQ_I8_MAX_COLUMNS.  For more than 64 tokens X and W on 16 bytes with row strides that are
- * multiples of 16 run fastest (a third of the time otherwise).  T == 0 is a no-op in both. */
+ * n <= REALQ_I8_MAX_COLUMNS.  For more than 16 tokens X and W on 16 bytes with row strides that are
+ * multiples of 16 run fastest (prompts take about three times as long otherwise).  T == 0 is a
+ * no-op in both. */
 #define REALQ_I8_MAX_COLUMNS 131071
 int realq_quantize_rows_i8(realq_ctx* ctx, const void* X, int32_t dtype, int64_t T, int64_t n, int64_t ldx, int8_t* Q,
                            int64_t ldq, float* scale);

@@ -116,3 +116,6 @@ def test_binding_refuses_before_the_call(monkeypatch):
         with pytest.raises(ValueError):
             call()
             pytest.fail(f"call {i} was taken")
+    for scale in (0.0, -1.0, float("nan")):
+        with pytest.raises(ValueError, match="scale"):
+            rq.packed_attention(ctx, q, k, k, cu, scale=scale)
