@@ -293,6 +293,9 @@ __device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64
 // maximum, sum and rescaling are the lane's own; only the maximum and the final sum cross to lane + 32.
 // O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
 // old one serves as well (P up to 256, exact to the same relative rounding).
+// Bound: the matrix unit beside the exponentials, with 2 waves a SIMD to fill either, at the clock that the board's
+// power leaves (8192 tokens, 32/8 heads x 128: 522 us, 1.05 PFLOP/s, MFMA busy 54% at 1.67 GHz; 4 x 2048: 160 us,
+// 0.86); few tiles: the longest block.
 template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
                                                                                        uint16_t* __restrict__ O,
@@ -433,7 +436,8 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
 // delta from the bf16 O is off by up to 2^-8 sum |O dO|, and dS is a small difference beside it where a softmax
 // has one large entry.  What it is off by is the sum of a row of dS (which is 0 for the true delta): that sum
 // goes into the delta stored for dK, and for the first tile of a sequence, whose rows see few keys (2 keys:
-// 6e-3 of dQ; 300: 2e-3), a pass over its keys forms delta as sum P dP first.
+// 6e-3 of dQ; 300: 2e-3), a pass over its keys forms delta as sum P dP first.  Bound: as the forward (8192 tokens,
+// 32/8 heads x 128: 724 us, 1.14 PFLOP/s of its 6 hd operations a pair, MFMA busy 60% at 1.68 GHz).
 template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
@@ -585,7 +589,10 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
 // sequence, which sets the time) any longer.  KL: K is read from LDS, which leaves 8 waves of 128 channels
 // their 256 registers; DK, DV: what this launch forms (both, or one each where both do not fit).  With splits > 1
 // a block takes one of that many shares of its tile's rounds and leaves float32 sums in `part`
-// ([split][dK, dV][T][n_kv hd]), which sum_splits_kernel adds in their order.
+// ([split][dK, dV][T][n_kv hd]), which sum_splits_kernel adds in their order.  S and dP are formed again, from what
+// the dQ kernel formed too: the one launch that forms them once would add dQ by atomics, in no fixed order.  Bound:
+// LDS reads and the matrix unit in turn (8192 tokens, 32/8 heads x 128: 1085 us, 1.01 PFLOP/s of its 8 hd operations
+// a pair, MFMA busy 49% at 1.81 GHz).
 template <int HD, int HC, int GROUPS, bool KL, bool DK, bool DV>
 __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,

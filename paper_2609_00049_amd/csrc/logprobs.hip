@@ -160,6 +160,8 @@ constexpr int CAP = 1024;  // candidates kept in LDS
 // a wave on each.  What passes is ranked by counting.  Keys are distinct, so ties cannot fill the list;
 // should more than CAP elements pass (or fewer than top: NaN), the stretch is searched once per alternative.
 // S == 1 writes the results; else the sums and keys go to `work`, and merge_kernel joins them.
+// Bound: reading the logits (4096 x 128256 bf16: 211 us, 5.0 TB/s; 2047 x 151936 with 5 alternatives: 4.9 TB/s, a
+// large copy's 5.3); one row alone: the chain of its steps, 16 us.
 template <class E, int BT, bool TOP>
 __global__ __launch_bounds__(BT) void scan_kernel(const E* __restrict__ Z, int64_t T, int64_t V, int64_t ld, int S,
                                                   int top, Out out, Acc4* __restrict__ part,
@@ -367,7 +369,8 @@ __global__ __launch_bounds__(64) void merge_kernel(const E* __restrict__ Z, int6
 
 // dz_j = -p_j (c + dH (log p_j + H)) + the incoming gradients of column j, c the sum of them all.
 // A block writes one stretch of a row, so the launch has enough of them whatever T is; logits and gradient
-// with the same offset to 16 bytes move in whole vectors.
+// with the same offset to 16 bytes move in whole vectors.  Bound: one read and one write of the array (4096 x 128256
+// bf16: 394 us, 5.3 TB/s); the rows go in the opposite order of the scan's, whose last ones the caches still hold.
 template <class E>
 __global__ __launch_bounds__(NT) void backward_kernel(const E* Z, int64_t T, int64_t V, int64_t ld, int64_t per_row,
                                                       const int64_t* __restrict__ targets, int top,
