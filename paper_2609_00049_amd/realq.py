@@ -700,6 +700,11 @@ class _Call:
 
     @staticmethod
     def _stride(t, name: str) -> int:
+        if t.dim() == 2:
+            step, inner = t.stride()
+            width = t.shape[1]
+            if inner == 1 and step >= width and t.shape[0] > 1:
+                return step
         width = 1
         for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
             if size > 1 and stride != width:
@@ -719,11 +724,17 @@ class _Call:
             raise ValueError(f"{name} must be contiguous")
         return self.rows(t, name, dtypes, shape)[0]
 
-    def new(self, shape, dtype) -> torch.Tensor:
-        if not self.foreign:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.ctx.stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+    def new(self, shape, dtype, ld: int = 0) -> torch.Tensor:
+        """An output or scratch tensor, contiguous or (2-d) with rows ld apart."""
+        if self.foreign:
+            with torch.cuda.stream(self.ctx.stream):
+                return self._new(shape, dtype, ld)
+        return self._new(shape, dtype, ld)
+
+    def _new(self, shape, dtype, ld):
+        if ld:
+            return torch.empty_strided(shape, (ld, 1), dtype=dtype, device=self.device)
+        return torch.empty(shape, dtype=dtype, device=self.device)
 
 
 _FLOAT, _BF, _F, _I8, _I64, _I32 = (BF16, F32), (BF16,), (F32,), (I8,), (I64,), (I32,)
@@ -848,10 +859,8 @@ def quantize_rows_i8(ctx: Context, X, out=None):
     x, ldx = call.rows(X, "X", _FLOAT, (T, n))
     if out is None:
         ldq = -(-n // 16) * 16
-        out = call.new((T, ldq), I8)
+        out = call.new((T, n), I8, ldq)
         q = out.data_ptr()
-        if ldq != n:
-            out = out[:, :n]
     else:
         q, ldq = call.rows(out, "out", _I8, (T, n))
     s = call.new((T,), F32)
