@@ -148,8 +148,9 @@ template <int N>
 __device__ __forceinline__ void vm_wait() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void block_sync() {  // LDS written by to_lds is visible once its writers have waited
-    asm volatile("" ::: "memory");
+// LDS written by to_lds is visible once its writers have waited; what was read is in registers and may be written
+__device__ __forceinline__ void block_sync() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
