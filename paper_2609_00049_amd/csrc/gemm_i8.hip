@@ -68,11 +68,23 @@ __device__ __forceinline__ i32x4 load16(const void* p) { return reinterpret_cast
 // columns k .. k + 15 of a row of n, zeros behind its end
 __device__ __forceinline__ i32x4 load_columns(const int8_t* p, int64_t k, int64_t n) {
     if (k + 16 <= n) return load16(p + k);
-    i32x4 v = {0, 0, 0, 0};
+    if (k >= n) return i32x4{0, 0, 0, 0};
+    struct {
+        uint64_t lo, hi;
+    } v = {0, 0};
+    if (n >= 16) {  // the row's last 16 bytes, less those before k: one load, not a chain of them
+        v = __builtin_bit_cast(decltype(v), load16(p + n - 16));
+        const int cut = 8 * (int)(k + 16 - n);  // 8 .. 120
+        v.lo = cut < 64 ? v.lo >> cut | v.hi << (64 - cut) : v.hi >> (cut - 64);
+        v.hi = cut < 64 ? v.hi >> cut : 0;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-        if (k + e < n) v[e >> 2] |= (int32_t)((uint32_t)(uint8_t)p[k + e] << (8 * (e & 3)));
-    return v;
+        for (int e = 0; e < 16; ++e) {
+            const uint64_t x = (uint8_t)p[min(k + e, n - 1)], y = k + e < n ? x : 0;
+            (e < 8 ? v.lo : v.hi) |= y << (8 * (e & 7));
+        }
+    }
+    return __builtin_bit_cast(i32x4, v);
 }
 
 constexpr int QT = 256;
@@ -373,8 +385,12 @@ __global__ __launch_bounds__(WM* WN* KG * 64, 2) void linear_i8_tile_kernel(
         rows[r] = sw[min(i0 + r, m - 1)];
         rows[BM + r] = bias ? bias[min(i0 + r, m - 1)] : 0.f;
     }
-    if (n % SL) {  // the last columns first, zeros behind them
-        const int64_t k0 = full * SL;
+    // the first slices' loads; the last stage is still free
+    for (int s = 0; s < NS - 1; ++s)
+        if (s < mine) issue(s, s);
+    if (n % SL) {  // the last columns, zeros behind them
+        int8_t* const rest = stages + (NS - 1) * STAGE;
+        const int64_t k0 = n / SL * SL;
         for (int c = threadIdx.x; c < (BM + BN) * 4; c += NT) {
             const int r = c >> 2;
             const bool w = r < BM;
@@ -382,11 +398,11 @@ __global__ __launch_bounds__(WM* WN* KG * 64, 2) void linear_i8_tile_kernel(
             const int8_t* p = w ? W + min(i0 + r, m - 1) * ldw : X + min(t0 + r - BM, T - 1) * ldx;
             const i32x4 v = load_columns(p, k, n);
             const int rr = w ? r : r - BM;
-            *reinterpret_cast<i32x4*>(stages + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
+            *reinterpret_cast<i32x4*>(rest + (w ? 0 : BM * SL) + rr * SL + 16 * chunk_at(rr, c & 3)) = v;
         }
         __syncthreads();
-        if (part == 0) multiply(stages);
-        __syncthreads();
+        if (part == 0) multiply(rest);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before a load refills the stage
     }
     if constexpr (NW == 8) {
         // Two waves share a SIMD, one of each group of 4.  Between two barriers one group multiplies a slice
@@ -427,8 +443,6 @@ __global__ __launch_bounds__(WM* WN* KG * 64, 2) void linear_i8_tile_kernel(
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         };
-        if (full > 0) issue(0, 0);
-        if (full > 1) issue(1, 1);
         if (full > 1) vm_wait<RA + RB>();
         else vm_wait<0>();
         __builtin_amdgcn_s_barrier();
@@ -445,12 +459,11 @@ __global__ __launch_bounds__(WM* WN* KG * 64, 2) void linear_i8_tile_kernel(
     } else {
         // slice s of the part: its loads have landed, everyone's are visible and nobody reads the stage of slice
         // s - 1 any more; NS - 1 slices are under way, so a slice waits for memory once in NS - 1
-        for (int s = 0; s < NS - 1; ++s)
-            if (s < mine) issue(s, s);
         int st = 0;
         for (int64_t s = 0; s < run; ++s) {
             if (s + NS - 2 < mine) vm_wait<(NS - 2) * (RA + RB)>();
             else vm_wait<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             const int before = st == 0 ? NS - 1 : st - 1;
             if (s + NS - 1 < mine) issue(s + NS - 1, before);
