@@ -87,7 +87,7 @@ def test_large_products(rq, ctx, T, n, m):
 
 
 @pytest.mark.parametrize("T,m", [(66, 1000), (90, 4000), (250, 3900), (300, 4000), (520, 5500), (3700, 2050)])
-@pytest.mark.parametrize("n", [1, 50, 64, 127, 128, 200, 450, 1090])
+@pytest.mark.parametrize("n", [1, 13, 50, 64, 127, 128, 200, 450, 1090])
 def test_numbers_of_tiles_and_slices(rq, ctx, T, m, n):
     """From a few tiles of outputs to many, over columns of less than a slice, one to seventeen and a rest."""
     g = gen(n + m)

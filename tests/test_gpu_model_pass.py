@@ -137,3 +137,35 @@ def test_another_stream(rq):
     del junk
     c.close()
     here.close()
+
+
+def test_two_contexts_at_once(rq):
+    """Two contexts on streams of their own, the same inputs and no wait between their calls."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn((500, 1000), generator=g, device="cuda").to(BF16)
+    w, sw = torch.randint(-127, 128, (900, 1000), generator=g, device="cuda").to(torch.int8), torch.rand(900, generator=g, device="cuda")
+    logits = torch.randn((3, 600000), generator=g, device="cuda")  # rows in stretches
+    y = torch.tensor([5, 599999, -1], device="cuda")
+    q = torch.randn((700, 4, 96), generator=g, device="cuda").to(BF16)
+    cu = torch.tensor([0, 100, 700], dtype=torch.int32, device="cuda")
+    ones = torch.ones(3, device="cuda")
+
+    def run(c):
+        s = rq.token_logprobs(c, logits, y, top=7, entropy=True)
+        o, lse = rq.packed_attention(c, q, q, q, cu)
+        return [rq.linear_i8(c, *rq.quantize_rows_i8(c, x), w, sw), s.lse, s.entropy, s.top_ids,
+                rq.token_logprobs_backward(c, logits, y, s, dlogp=ones, dentropy=ones), o, lse,
+                *rq.packed_attention_backward(c, q, q, q, cu, o, lse, q)]
+
+    torch.cuda.synchronize()
+    contexts = [rq.Context(torch.cuda.Stream()) for _ in range(2)]
+    want = run(contexts[0])
+    torch.cuda.synchronize()
+    got = [[run(c) for c in contexts] for _ in range(4)]
+    torch.cuda.synchronize()
+    for pair in got:
+        for outs in pair:
+            for a, b in zip(outs, want):
+                assert torch.equal(a, b)
+    for c in contexts:
+        c.close()
