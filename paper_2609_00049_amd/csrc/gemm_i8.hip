@@ -239,14 +239,25 @@ __global__ __launch_bounds__(256) void linear_i8_kernel(const int8_t* __restrict
     auto load = [&](const int8_t* P, int64_t ld, int64_t rows, int64_t r, int64_t k) {
         return r < rows ? load_columns(P + r * ld, k, n) : i32x4{0, 0, 0, 0};
     };
+    i32x4 next[2][2];  // a slice on its way while the one before is multiplied
+    auto fetch = [&](int64_t k0) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int ch = threadIdx.x + c * 256, r = ch >> 2, kc = (ch & 3) * 16;
+            next[0][c] = load(W, ldw, m, i0 + r, k0 + kc);
+            next[1][c] = load(X, ldx, T, t0 + r, k0 + kc);
+        }
+    };
+    fetch(0);
     for (int64_t k0 = 0; k0 < n; k0 += SK) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int ch = threadIdx.x + c * 256, r = ch >> 2, kc = (ch & 3) * 16;
-            *reinterpret_cast<i32x4*>(sa + r * SLD + kc) = load(W, ldw, m, i0 + r, k0 + kc);
-            *reinterpret_cast<i32x4*>(sb + r * SLD + kc) = load(X, ldx, T, t0 + r, k0 + kc);
+            *reinterpret_cast<i32x4*>(sa + r * SLD + kc) = next[0][c];
+            *reinterpret_cast<i32x4*>(sb + r * SLD + kc) = next[1][c];
         }
         __syncthreads();
+        if (k0 + SK < n) fetch(k0 + SK);
 #pragma unroll
         for (int kk = 0; kk < SK; kk += 32) {
             i32x4 a[2], b[2];
