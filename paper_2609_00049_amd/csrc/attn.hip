@@ -15,6 +15,7 @@
 // indices.
 #include "common.h"
 #include "kernels.h"
+#include "to_lds.h"
 
 namespace realq {
 
@@ -282,14 +283,6 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(const uint16_t* __restric
 //   key tile   [32 keys][HD] bf16, chunk c of key row r at position c ^ (r mod HD/8)
 //   value tile [HD cols][32 keys] bf16 (from v^T), chunk c of row r at c ^ ((r/2 ^ r/8) mod 4)
 namespace {
-__device__ __forceinline__ void attn_dma16(const void* sbase, uint32_t voff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
-                 : "memory", "m0");
-}
-template <int N>
-__device__ __forceinline__ void attn_wait_vm() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ int vswz(int r) { return ((r >> 1) ^ (r >> 3)) & 3; }
 // hi | lo << 16 of one value, and the three bf16 terms of eight, rounded by the conversion instruction (to nearest even, as f2bf).
 __device__ __forceinline__ uint32_t split_pk(float x) {
@@ -350,7 +343,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_lds_kernel(const uint16_t* __
             const int qi = wv * KDMA + q;                    // 1 KB piece of the tile
             const int row = qi * (1024 / (HD * 2)) + lane / KCH, pos = lane % KCH;
             const int c = pos ^ (row % KCH);
-            attn_dma16(kb, (uint32_t)((row * ldk + c * 8) * 2), kd + (uint32_t)qi * 1024);
+            to_lds(kb, (uint32_t)((row * ldk + c * 8) * 2), kd + (uint32_t)qi * 1024);
         }
         if (with_v) {
             const char* vb = reinterpret_cast<const char*>(vbase + jt * AT);
@@ -359,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_lds_kernel(const uint16_t* __
                 const int qi = wv * VDMA + q;
                 const int row = qi * 16 + (lane >> 2), pos = lane & 3;
                 const int c = pos ^ vswz(row);
-                attn_dma16(vb, (uint32_t)((row * T + c * 8) * 2), kd + KBYTES + (uint32_t)qi * 1024);
+                to_lds(vb, (uint32_t)((row * T + c * 8) * 2), kd + KBYTES + (uint32_t)qi * 1024);
             }
         }
     };
@@ -392,7 +385,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_lds_kernel(const uint16_t* __
     double m_row = -1e300, l_row = 0.0;    // of this half lane's keys (finite: it may have none)
     load_tile(0, 0, false);
     for (int64_t jt = 0; jt <= itmax; ++jt) {
-        attn_wait_vm<0>();                 // this wave's share of tile jt has landed
+        vm_wait<0>();                 // this wave's share of tile jt has landed
         __syncthreads();                   // every share landed; tile jt-1's buffer is free
         if (jt + 1 <= itmax) load_tile(jt + 1, (int)((jt + 1) & 1), false);
         if (jt <= it) {
@@ -426,11 +419,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_lds_kernel(const uint16_t* __
     f32x16 oacc[NCT];
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) oacc[ct] = zero16();
-    attn_wait_vm<0>();
+    vm_wait<0>();
     __syncthreads();                       // pass 1's reads of both buffers are done
     load_tile(0, 0, true);
     for (int64_t jt = 0; jt <= itmax; ++jt) {
-        attn_wait_vm<0>();
+        vm_wait<0>();
         __syncthreads();
         if (jt + 1 <= itmax) load_tile(jt + 1, (int)((jt + 1) & 1), true);
         if (jt <= it) {
@@ -647,8 +640,8 @@ __global__ __launch_bounds__(256) void attn_ds_lds_kernel(const uint16_t* __rest
             const int qi = wv * TDMA + q;
             const int row = qi * (1024 / (HD * 2)) + lane / KCH, pos = lane % KCH;
             const uint32_t off = (uint32_t)((row * ldk + (pos ^ (row % KCH)) * 8) * 2);
-            attn_dma16(kb, off, dst + (uint32_t)qi * 1024);
-            attn_dma16(vb, off, dst + TBYTES + (uint32_t)qi * 1024);
+            to_lds(kb, off, dst + (uint32_t)qi * 1024);
+            to_lds(vb, off, dst + TBYTES + (uint32_t)qi * 1024);
         }
     };
     // this wave's rows: query fragments (LDS), dO (registers, split once into its three bf16
@@ -710,8 +703,8 @@ __global__ __launch_bounds__(256) void attn_ds_lds_kernel(const uint16_t* __rest
     for (int64_t jt = 0; jt <= itmax; ++jt) {
         // this wave's loads of tile jt have landed; the 12 stores of the previous tile, issued after
         // those loads, may still be in flight
-        if (jt >= 1 && jt - 1 <= it) attn_wait_vm<12>();
-        else attn_wait_vm<0>();
+        if (jt >= 1 && jt - 1 <= it) vm_wait<12>();
+        else vm_wait<0>();
         __syncthreads();
         if (jt + 1 <= itmax) load_tile(jt + 1, (int)((jt + 1) & 1));
         if (jt > it) continue;

@@ -19,6 +19,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "to_lds.h"
 
 namespace realq {
 
@@ -139,22 +140,12 @@ __device__ __forceinline__ Seq find_tile(const int32_t* __restrict__ cu, int64_t
     return s;
 }
 
-// Lane i fills LDS bytes lds + 16 i .. + 15 from base + its own byte offset; completion is waited for by
-// vm_wait, not by the compiler.
-__device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
-}
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 // LDS written by to_lds is visible once its writers have waited; what was read is in registers and may be written
 __device__ __forceinline__ void block_sync() {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)p; }
 
 // Brings rows r0 .. r0 + ROWS - 1 of one head (past the sequence's last one: that one again) into an LDS
 // tile by direct-to-LDS loads, NW waves sharing the work.  Channels from hd on are not touched: the tile is

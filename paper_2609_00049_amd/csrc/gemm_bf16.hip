@@ -28,6 +28,7 @@
 #include "common.h"
 #include "kernels.h"
 #include "plan.h"
+#include "to_lds.h"
 
 namespace realq {
 
@@ -101,21 +102,7 @@ __device__ __forceinline__ bf16x8 frag(const uint16_t* lds, int row, int k) {
                               *reinterpret_cast<const u16x8*>(lds + row * LDS_STRIDE + swz(row, k >> 3) * 8));
 }
 
-// 16-byte direct-to-LDS load: lane i reads sbase + voff (its own 32-bit byte offset) and
-// fills LDS bytes [lds + 16i, lds + 16i + 16) (lds is wave-uniform).  Issued as inline
-// assembly so the compiler does not insert conservative waits for it; every consumer is
-// ordered by the explicit vmcnt waits and barriers of the K loop.
-__device__ __forceinline__ void dma16(const void* sbase, uint32_t voff, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
-                 : "memory", "m0");
-}
-template <int N>
-__device__ __forceinline__ void wait_vmcnt() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void wait_lgkm0() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-// LDS byte address of a __shared__ object: the low 32 bits of its generic address.
-__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)p; }
 
 // Tile coordinates of block b: XCD-contiguous renumbering, then grouped row-tile order.
 __device__ __forceinline__ void tile_of_v(int64_t b, int64_t tiles_m, int64_t tiles_n, int64_t group_m, int64_t& tm,
@@ -227,24 +214,24 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
     const char* const baseA = reinterpret_cast<const char*>(Ahi + m0 * lda + (kbeg << a_sh));
     const char* const baseAl = HAS_LO ? reinterpret_cast<const char*>(Alo + m0 * lda + (kbeg << a_sh)) : baseA;
     const char* const baseB = reinterpret_cast<const char*>(B + n0 * ldb + kbeg);
-    const uint32_t lds_st[3] = {lds_addr(st0), lds_addr(st1), lds_addr(st2)};
+    const uint32_t lds_st[3] = {lds_at(st0), lds_at(st1), lds_at(st2)};
     auto issue = [&](int64_t s, uint32_t stage) {
         const int64_t off = s * BK * 2;
         const int64_t offa = s * a_step;
 #pragma unroll
         for (int q = 0; q < A_RUNS; ++q) {
             const uint32_t d = stage + (uint32_t)((wv + NW * q) * 16 * LDS_STRIDE * 2);
-            dma16(baseA + offa, offA[q], d);
-            if constexpr (HAS_LO) dma16(baseAl + offa, offA[q], d + C::BM * LDS_STRIDE * 2);
+            to_lds(baseA + offa, offA[q], d);
+            if constexpr (HAS_LO) to_lds(baseAl + offa, offA[q], d + C::BM * LDS_STRIDE * 2);
         }
 #pragma unroll
         for (int q = 0; q < B_RUNS; ++q)
-            dma16(baseB + off, offB[q], stage + (uint32_t)((A_ROWS + (wv + NW * q) * 16) * LDS_STRIDE * 2));
+            to_lds(baseB + off, offB[q], stage + (uint32_t)((A_ROWS + (wv + NW * q) * 16) * LDS_STRIDE * 2));
     };
     // wait until at most n direct-to-LDS loads of this wave are outstanding
     auto wait_vm = [](int n) {
-        if (n >= DMA_PER_SLICE) wait_vmcnt<DMA_PER_SLICE>();
-        else wait_vmcnt<0>();
+        if (n >= DMA_PER_SLICE) vm_wait<DMA_PER_SLICE>();
+        else vm_wait<0>();
     };
     struct Frags {
         bf16x8 a[C::SM], al[HAS_LO ? C::SM : 1], b[C::SN];
@@ -308,13 +295,13 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
             load_frags(cur, 16, f1);
             if (s + 2 < nfull) issue(s + 2, fill);
             wait_lgkm0();
-            if (s + 2 < nfull) wait_vmcnt<DMA_PER_SLICE>();
-            else wait_vmcnt<0>();
+            if (s + 2 < nfull) vm_wait<DMA_PER_SLICE>();
+            else vm_wait<0>();
         };
         if (nfull > 0) issue(0, lds_st[0]);
         if (nfull > 1) issue(1, lds_st[1]);
-        if (nfull > 1) wait_vmcnt<DMA_PER_SLICE>();
-        else wait_vmcnt<0>();
+        if (nfull > 1) vm_wait<DMA_PER_SLICE>();
+        else vm_wait<0>();
         __builtin_amdgcn_s_barrier();
         if (grp == 1) __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -360,7 +347,7 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
     }
 #undef RQ_STEP
     }
-    wait_vmcnt<0>();
+    vm_wait<0>();
     __syncthreads();
     for (int64_t s = nfull; s < nk; ++s) {  // checked tail, single-buffered in stage 0
         const int64_t k0 = kbeg + s * BK;
@@ -412,7 +399,7 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
             const int64_t ldb0 = epi.row_ld();
             uint16_t* const ring16 = (wv < 4 ? st1 : st2) + (wv & 3) * (RING * 2048);
             const float* const ring = reinterpret_cast<const float*>(ring16);
-            const uint32_t ring_lds = lds_addr(ring16);
+            const uint32_t ring_lds = lds_at(ring16);
             auto dma_sub = [&](int t) {
                 const int64_t r0 = m0 + wms * C::WTM + (t / C::SN) * 32;
                 const int64_t c0 = n0 + wns * C::WTN + (t % C::SN) * 32;
@@ -420,7 +407,7 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
                 const uint32_t slot = ring_lds + (uint32_t)((t % RING) * 4096);
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    dma16(base, (uint32_t)(((int64_t)(q * 8 + (lane >> 3)) * ldb0 + (lane & 7) * 4) * 4),
+                    to_lds(base, (uint32_t)(((int64_t)(q * 8 + (lane >> 3)) * ldb0 + (lane & 7) * 4) * 4),
                           slot + q * 1024);
             };
             // vector-memory operations of this lane issued after sub-tile t's streamed loads, at the
@@ -441,11 +428,11 @@ __global__ __launch_bounds__(C::NT) void gemm_nt_kernel(const uint16_t* __restri
 #pragma unroll
             for (int t = 0; t < NSUB; ++t) {
                 switch (after(t)) {  // constant after unrolling
-                    case 8: wait_vmcnt<8>(); break;
-                    case 16: wait_vmcnt<16>(); break;
-                    case 20: wait_vmcnt<20>(); break;
-                    case 24: wait_vmcnt<24>(); break;
-                    default: wait_vmcnt<0>(); break;
+                    case 8: vm_wait<8>(); break;
+                    case 16: vm_wait<16>(); break;
+                    case 20: vm_wait<20>(); break;
+                    case 24: vm_wait<24>(); break;
+                    default: vm_wait<0>(); break;
                 }
                 const int i = t / C::SN, j = t % C::SN;
 #pragma unroll

@@ -8,6 +8,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "to_lds.h"
 
 namespace realq {
 
@@ -302,16 +303,6 @@ namespace {
 constexpr int SL = 64;  // columns (bytes) of a slice
 
 __device__ __forceinline__ int chunk_at(int r, int c) { return (c ^ ((r >> 1) ^ (r >> 3))) & 3; }
-// lane i fills LDS bytes lds + 16 i .. + 15 from base + its own byte offset; completion is waited for by the
-// vmcnt counts of the K loop, not by the compiler
-__device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
-}
-template <int N>
-__device__ __forceinline__ void vm_wait() {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_at(const void* p) { return (uint32_t)(uintptr_t)p; }
 
 // Tile of block b: each XCD (blocks are dealt to the 8 round-robin) owns one run of tiles, walked in bands of
 // `band` weight tiles so that a band's weights and a few token tiles stay in its L2.
