@@ -603,8 +603,11 @@ int realq_token_logprobs_backward(realq_ctx* ctx, const realq_logprobs_desc* des
  *
  * realq_packed_attention_backward: from dO, dQ (like q), dK and dV (like k, v; summed over the query
  * heads that share them), rows lddq / lddk / lddv apart, bf16, by the formulas
- *   dV = P^T dO,  dS = P (dO v^T - delta),  delta_i = sum O_i dO_i,  dQ = scale dS k,  dK = scale dS^T q;
- * O and lse as the forward call gave them; work: scratch memory of at least
+ *   dV = P^T dO,  dS = P (dO v^T - delta),  delta_i = sum O_i dO_i,  dQ = scale dS k,  dK = scale dS^T q,
+ * where delta is not left to the rounding of O: its error goes by float32 in dK, and in dQ it is at most 2^-9 of the
+ * row's sum of |dS| (tiles with rows of one large P take a
+ * second pass over their keys: up to 1.4 times as long).  O and lse as the forward
+ * call gave them; work: scratch memory of at least
  * realq_packed_attention_workspace bytes (by T, n_seqs, the heads and head_dim; the arrays are not looked
  * at), aligned to 16, which needs no clearing.  The sums have an order fixed by the sizes (T, n_seqs, the heads,
  * head_dim): the same call gives the same bits.  Outputs must not overlap inputs or each other

@@ -427,9 +427,12 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
 // forward a query's scores are one lane's: S^T = K Q^T, dP^T = V dO^T, and dS^T goes into dQ^T += K^T dS^T.
 // delta from the bf16 O is off by up to 2^-8 sum |O dO|, and dS is a small difference beside it where a softmax
 // has one large entry.  What it is off by is the sum of a row of dS (which is 0 for the true delta): that sum
-// goes into the delta stored for dK, and for the first tile of a sequence, whose rows see few keys (2 keys:
-// 6e-3 of dQ; 300: 2e-3), a pass over its keys forms delta as sum P dP first.  Bound: as the forward (8192 tokens,
-// 32/8 heads x 128: 724 us, 1.14 PFLOP/s of its 6 hd operations a pair, MFMA busy 60% at 1.68 GHz).
+// goes into the delta stored for dK, and waves with a row where it passes 2^-9 of the row's sum of |dS| (half of what
+// the rounding of dS to bf16 may move) form dQ once more with the true delta.  Without that, rows with a sink of P
+// near 1 were off by more than their own size (600 tokens x 64 channels); with it by 0.01 of it at most.  The first
+// tile of a sequence, whose rows see few keys, forms delta as sum P dP in a pass of its own before.  Bound: as the
+// forward (8192 tokens, 32/8 heads x 128: 772 us, 1.07 PFLOP/s of its 6 hd operations a pair; 1394 us where every
+// wave takes the second pass).
 template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
@@ -437,12 +440,14 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
     int64_t tiles) {
     constexpr int BN = HD <= 128 ? 64 : 32;
     __shared__ __attribute__((aligned(16))) uint16_t all_lds[GROUPS][2][2][BN * HD];
-    __shared__ float sums[GROUPS][BM];
+    __shared__ float sums[2][GROUPS][BM];
+    __shared__ int again;
     int64_t rank;
     int h;
     item_of(a.n_heads, rank, h);
     const Seq sq = ranked_tile<BM, false>(a.cu, a.n_seqs, a.T, tiles, rank);
     if (!sq.any) return;
+    if (threadIdx.x == 0) again = 0;  // read behind the passes' barriers
     const int kv = h / (a.n_heads / a.n_kv);
     const int lane = threadIdx.x & 63, tid = threadIdx.x & 255;
     const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = all >> 2, wave = all & 3;
@@ -461,7 +466,6 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
             loader.load(V, a.ldv, grp * BN, sq.len, lds_at(kv_lds[0][1]));
         }
     };
-    begin();
     bf16x8 qf[HC / 16], df[HC / 16];
     hold<HC>(a.q + row * a.ldq + h * a.hd, a.hd, lane, qf);
     hold<HC>(dO + row * lddo + h * a.hd, a.hd, lane, df);
@@ -480,8 +484,13 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
     f32x16 g[HC / 32];
 #pragma unroll
     for (int t = 0; t < HC / 32; ++t) g[t] = zero16();
-    float sum = 0.f;  // of this lane's part of the row of P dP, then of dS
+    // Of this lane's part of the row: the sum of dS (first of P dP), and of the magnitudes of its sums over 16 keys,
+    // which is at most that of |dS| and near it where few entries are large.
+    float sum = 0.f, size = 0.f, off = 0.f;
+    bool mine = true;  // the wave takes part
     auto sweep = [&](bool products) {
+        sum = size = 0.f;
+        begin();
         alternate(grp * BN, keys + grp * BN, GROUPS * BN, [&](auto buffer, int k0) {
             constexpr int buf = decltype(buffer)::value;
             vm_wait<0>();
@@ -491,6 +500,7 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                 loader.load(K, a.ldk, next, sq.len, lds_at(kv_lds[buf ^ 1][0]));
                 loader.load(V, a.ldv, next, sq.len, lds_at(kv_lds[buf ^ 1][1]));
             }
+            if (!mine) return;
             const uint16_t* sk = kv_lds[buf][0];
             const uint16_t* sv = kv_lds[buf][1];
 #pragma unroll
@@ -510,9 +520,11 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                         if (kb + crow(e, lane) > qi || qi == 0) s[e] = -INFINITY;  // one key: dS is 0
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -L)) * (dp[e] - dl);
-                sum += (((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) +
-                       (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));
+                const float part = (((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) +
+                                   (((s[8] + s[9]) + (s[10] + s[11])) + ((s[12] + s[13]) + (s[14] + s[15])));
+                sum += part;
                 if (!products) continue;
+                size += fabsf(part);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const bf16x8 d = pack_frag(s, x);
@@ -521,27 +533,40 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
                 }
             }
         });
-    };
-    // the sum over both halves of the wave and both groups, in every lane of the query
-    auto whole = [&]() {
-        float x = sum + other_half(sum);
-        sum = 0.f;
+        // over both halves of the wave and both groups, in every lane of the query
+        sum += other_half(sum);
+        size += other_half(size);
         if constexpr (GROUPS == 2) {
-            if (lane < 32) sums[grp][wave * 32 + lane] = x;
+            if (lane < 32) {
+                sums[0][grp][wave * 32 + lane] = sum;
+                sums[1][grp][wave * 32 + lane] = size;
+            }
             __syncthreads();
-            x = sums[0][wave * 32 + (lane & 31)] + sums[1][wave * 32 + (lane & 31)];
+            sum = sums[0][0][wave * 32 + (lane & 31)] + sums[0][1][wave * 32 + (lane & 31)];
+            size = sums[1][0][wave * 32 + (lane & 31)] + sums[1][1][wave * 32 + (lane & 31)];
         }
-        __syncthreads();  // the tiles' LDS is free again
-        return x;
     };
     if (sq.tile == 0) {
         dl = 0.f;
         sweep(false);
-        dl = whole();
-        begin();
+        dl = sum;
+        __syncthreads();  // the tiles' LDS is free again
     }
     sweep(true);
-    const float off = whole();
+    off = sum;
+    mine = __any(live && fabsf(off) > 0x1p-9f * size);
+    if (mine && lane == 0) again = 1;
+    __syncthreads();  // the tiles' LDS is free again
+    if (again) {
+        if (mine) {
+            dl += off;
+#pragma unroll
+            for (int t = 0; t < HC / 32; ++t) g[t] = zero16();
+        }
+        sweep(true);
+        if (mine) off = sum;
+        __syncthreads();
+    }
     if (live && grp == 0 && lane < 32) delta[(int64_t)h * a.T + row] = dl + off;
     if constexpr (GROUPS == 2) {
         float* const sh = reinterpret_cast<float*>(all_lds[0][0][0]) + tid;
