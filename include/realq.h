@@ -552,6 +552,8 @@ int realq_decoder_forward(realq_ctx* ctx, const realq_decoder_desc* desc, realq_
  * ld >= V, bf16 or float32), in float32 throughout:
  *   lse      = log sum_j e^z_j                                     [T], required
  *   logp     = z_y - lse for the row's target y                    [T] | NULL (needs targets)
+ *              (as (z_y - max z) - log sum e^(z - max z), top_logp too: an offset common to a
+ *              row's logits costs them no digits, while lse is rounded at its own size)
  *   entropy  = -sum_j p_j log p_j,  p_j = e^(z_j - lse)            [T] | NULL
  *   top_ids, top_logp: the `top` largest logits' columns and log probabilities, larger first, equal
  *              logits (-0 equals 0) by the lower column            [T, top], required when top > 0
@@ -569,7 +571,8 @@ int realq_decoder_forward(realq_ctx* ctx, const realq_decoder_desc* desc, realq_
  * the given derivatives with respect to logp [T], entropy [T] and top_logp [T, top] (each may be NULL):
  *   dz_j = -p_j (c + dentropy (log p_j + entropy)) + [j = y] dlogp + sum_k [j = top_ids_k] dtop_k,
  *   c = dlogp + sum_k dtop_k,
- * rounded once.  lse, entropy and top_ids as the forward call gave them (entropy only with
+ * rounded once; p from the float32 lse, so relative to it off by up to 2^-24 |lse| too.  lse, entropy and
+ * top_ids as the forward call gave them (entropy only with
  * dentropy, top_ids only with dtop; a column listed more than once receives the sum, one outside
  * 0 .. V-1 nothing).  A target below 0 takes no part; one of V or more makes its row NaN where
  * dlogp is given; an empty row's gradient is 0. */

@@ -3,9 +3,10 @@
 //
 // One pass over the logits z of a row keeps, per thread, the running maximum m and
 //     S = sum e^(z - m),   U = sum e^(z - m) (z - m),
-// from which lse = m + log S, logp_j = z_j - lse and the entropy is log S - U / S (differences to the
-// maximum throughout: no large terms cancel).  All of it is float32; a row with no finite logit keeps
-// S = 0 and is an empty row.
+// from which lse = m + log S, logp_j = (z_j - m) - log S and the entropy is log S - U / S (differences to the
+// maximum throughout: no large terms cancel, and an offset common to a row's logits costs no digits; only lse,
+// which is rounded at its own size, and the gradient, which starts from it, feel one).  All of it is float32; a
+// row with no finite logit keeps S = 0 and is an empty row.
 #include <algorithm>
 
 #include "common.h"
@@ -126,7 +127,7 @@ __device__ __forceinline__ Acc wave_merge(Acc a) {
     return a;
 }
 
-// Results of a row from its merged sums (one thread).
+// Results of a row from its merged sums (one thread); returns log S.
 template <class E>
 __device__ __forceinline__ float finish(const Acc& a, const E* z, int64_t V, int64_t t, const Out& o) {
     const float logs = logf(a.s);
@@ -138,14 +139,15 @@ __device__ __forceinline__ float finish(const Acc& a, const E* z, int64_t V, int
         const int64_t y = o.targets[t];
         float r = 0.f;
         if (y >= V) r = NAN;
-        else if (y >= 0) r = empty ? -INFINITY : value(z[y]) - l;
+        else if (y >= 0) r = empty ? -INFINITY : (value(z[y]) - a.m) - logs;
         o.logp[t] = r;
     }
-    return l;
+    return logs;
 }
-__device__ __forceinline__ void put_top(uint64_t key, float l, int64_t at, const Out& o) {
+// m and logs of the row; log S is -infinity in an empty one
+__device__ __forceinline__ void put_top(uint64_t key, float m, float logs, int64_t at, const Out& o) {
     o.top_ids[at] = column_of(key);
-    o.top_logp[at] = l == -INFINITY ? -INFINITY : value_of(key) - l;
+    o.top_logp[at] = logs == -INFINITY ? -INFINITY : (value_of(key) - m) - logs;
 }
 
 constexpr int CAP = 1024;  // candidates kept in LDS
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(BT) void scan_kernel(const E* __restrict__ Z, int64
     __shared__ uint64_t group[64], cand[TOP ? CAP : 1];
     __shared__ uint64_t bound;
     __shared__ int count;
-    __shared__ float row_lse;
+    __shared__ float row_max, row_logs;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int64_t item = blockIdx.x; item < T * S; item += gridDim.x) {
         const int64_t t = S == 1 ? item : item / S;
@@ -251,8 +253,12 @@ __global__ __launch_bounds__(BT) void scan_kernel(const E* __restrict__ Z, int64
         __syncthreads();
         if (tid == 0) {
             for (int w = 1; w < BT / 64; ++w) merge(a, wacc[w]);
-            if (S == 1) row_lse = finish(a, row.z, V, t, out);
-            else part[item] = {a.m, a.s, a.u, 0.f};
+            if (S == 1) {
+                row_max = a.m;
+                row_logs = finish(a, row.z, V, t, out);
+            } else {
+                part[item] = {a.m, a.s, a.u, 0.f};
+            }
         }
         if constexpr (TOP) {
             if (wave == 1) {
@@ -290,10 +296,10 @@ __global__ __launch_bounds__(BT) void scan_kernel(const E* __restrict__ Z, int64
             const int c = count;
             const int64_t here = (v1 - v0) * N + e0 + e1;
             const int want = (int)min((int64_t)top, here);
-            const float l = S == 1 ? row_lse : 0.f;
+            const float m = S == 1 ? row_max : 0.f, logs = S == 1 ? row_logs : 0.f;
             uint64_t* const mine = S == 1 ? nullptr : keys + item * top;
             auto emit = [&](uint64_t k, int r) {
-                if (S == 1) put_top(k, l, t * top + r, out);
+                if (S == 1) put_top(k, m, logs, t * top + r, out);
                 else mine[r] = k;
             };
             if (c <= CAP && c >= want) {
@@ -350,7 +356,7 @@ __global__ __launch_bounds__(64) void merge_kernel(const E* __restrict__ Z, int6
             a = {p.m, p.s, p.u};
         }
         a = wave_merge(a);
-        const float l = __shfl(lane == 0 ? finish(a, Z + t * ld, V, t, out) : 0.f, 0);
+        const float m = __shfl(a.m, 0), logs = __shfl(lane == 0 ? finish(a, Z + t * ld, V, t, out) : 0.f, 0);
         __syncthreads();
         int next = 0;
         uint64_t head = lane < S && top ? sh[lane * top] : 0, got = 0;
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(64) void merge_kernel(const E* __restrict__ Z, int6
                 head = next < top ? sh[lane * top + next] : 0;
             }
         }
-        if (lane < top) put_top(got, l, t * top + lane, out);
+        if (lane < top) put_top(got, m, logs, t * top + lane, out);
         __syncthreads();
     }
 }
