@@ -17,11 +17,13 @@ _KEPT = {}
 
 
 def _lib():
-    """The binding and this process's Context (only where `own` is set)."""
-    if not _KEPT:
+    """The binding and the Context of the current stream (only where `own` is set)."""
+    device = torch._C._cuda_getDevice()
+    key = device, torch._C._cuda_getCurrentRawStream(device)  # without making a Stream object
+    if key not in _KEPT:
         from paper_2609_00049_amd import realq
-        _KEPT["rq"], _KEPT["ctx"] = realq, realq.Context()
-    return _KEPT["rq"], _KEPT["ctx"]
+        _KEPT[key] = realq, realq.Context(torch.cuda.current_stream())
+    return _KEPT[key]
 
 
 # ----------------------------------------------------------------------------- the cases
