@@ -804,8 +804,9 @@ def _attention_desc(call: _Call, q, k, v, cu_seqlens, scale):
     (B,) = _dims(cu_seqlens, "cu_seqlens", 1)
     if B < 1:
         raise ValueError("cu_seqlens must hold at least one offset")
-    if scale is not None and not scale > 0:
-        raise ValueError(f"scale must be above 0, got {scale}")
+    # as the C ABI receives it, where 0 stands for the default
+    if scale is not None and not ctypes.c_float(scale).value > 0:
+        raise ValueError(f"scale must be above 0 in float32, got {scale}")
     pq, ldq = call.rows(q, "q", _BF, (T, H, hd))
     pk, ldk = call.rows(k, "k", _BF, (T, G, hd))
     pv, ldv = call.rows(v, "v", _BF, (T, G, hd))

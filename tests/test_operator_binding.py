@@ -1,0 +1,35 @@
+"""Calls of the operators that the binding has to refuse or prepare itself, without a GPU."""
+import types
+
+import pytest
+import torch
+
+from paper_2609_00049_amd import realq as rq
+
+B = torch.bfloat16
+
+
+@pytest.fixture
+def ctx(monkeypatch):
+    """A context whose tensors are on the host and whose calls into the C ABI fail the test."""
+    def called(*args):
+        raise AssertionError("the C ABI was called")
+
+    monkeypatch.setattr(rq, "_current", lambda i: 0)
+    monkeypatch.setattr(rq, "_lib", types.SimpleNamespace(**{n: called for n in rq.EXPORTS}))
+    return types.SimpleNamespace(h=None, device=torch.device("cpu"), raw_stream=0, check=called)
+
+
+def heads():
+    return torch.zeros((6, 4, 64), dtype=B), torch.zeros((6, 2, 64), dtype=B), torch.tensor([0, 6], dtype=torch.int32)
+
+
+@pytest.mark.parametrize("scale", [1e-50, 1e-46, -1e-50])
+def test_a_scale_that_is_no_float32_above_zero(ctx, scale):
+    """It would arrive as 0, which stands for the default."""
+    q, k, cu = heads()
+    lse = torch.zeros((4, 6))
+    with pytest.raises(ValueError, match="scale"):
+        rq.packed_attention(ctx, q, k, k, cu, scale=scale)
+    with pytest.raises(ValueError, match="scale"):
+        rq.packed_attention_backward(ctx, q, k, k, cu, q, lse, q, scale=scale)
