@@ -262,7 +262,8 @@ class Context:
         self.stream = stream
         self.device, self.raw_stream = stream.device, stream.cuda_stream
         h = ctypes.c_void_p()
-        rc = _lib.realq_ctx_create(ctypes.byref(h), ctypes.c_void_p(stream.cuda_stream))
+        with torch.cuda.device(stream.device):  # the C ABI binds a context to the current device
+            rc = _lib.realq_ctx_create(ctypes.byref(h), ctypes.c_void_p(stream.cuda_stream))
         if rc != OK:
             raise RealqError(rc, "realq_ctx_create failed")
         self.h = h

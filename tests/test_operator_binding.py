@@ -1,4 +1,5 @@
-"""Calls of the operators that the binding has to refuse or prepare itself, without a GPU."""
+"""Contexts and calls of the operators that the binding has to refuse or prepare itself, without a GPU."""
+import contextlib
 import types
 
 import pytest
@@ -33,3 +34,23 @@ def test_a_scale_that_is_no_float32_above_zero(ctx, scale):
         rq.packed_attention(ctx, q, k, k, cu, scale=scale)
     with pytest.raises(ValueError, match="scale"):
         rq.packed_attention_backward(ctx, q, k, k, cu, q, lse, q, scale=scale)
+
+
+def test_a_context_is_created_on_its_streams_device(monkeypatch):
+    """The C ABI binds a context to the device that is current, which need not be the stream's."""
+    current, seen = [torch.device("cuda:0")], []
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], torch.device(d)
+        yield
+        current[0] = before
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(rq, "_lib", types.SimpleNamespace(
+        realq_ctx_create=lambda h, stream: seen.append(current[0]) or 0, realq_ctx_destroy=lambda h: None))
+    for name in ("cuda:1", "cuda:0"):
+        c = rq.Context(types.SimpleNamespace(device=torch.device(name), cuda_stream=5))
+        assert seen[-1] == c.device == torch.device(name)
+        c.close()
+    assert current[0] == torch.device("cuda:0")
