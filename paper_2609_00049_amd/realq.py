@@ -661,6 +661,8 @@ def decoder_forward(ctx: Context, X, blk: dict, *, n_heads, n_kv, head_dim, seq_
 #
 # Work goes on the context's stream, scratch memory and outputs that are not given come from torch's
 # allocator on that stream.  Rows may be strided (a slice of a wider tensor); the last axis is contiguous.
+# Results carry no graph: a tensor that requires grad is refused while torch records one (in the forward and the
+# backward of a torch.autograd.Function it does not), so that no gradient is lost silently.
 
 I8, I64, I32 = torch.int8, torch.int64, torch.int32
 LOGPROBS_MAX_TOP = 64
@@ -695,6 +697,9 @@ class _Call:
             ld = self._stride(t, name)
         if t.device != self.device:
             raise ValueError(f"{name} must be on {self.device}, got {t.device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires grad, which these calls do not record: detach it, or call under "
+                             "torch.no_grad() or from a torch.autograd.Function")
         if self.foreign:
             t.record_stream(self.ctx.stream)
         return t.data_ptr(), ld

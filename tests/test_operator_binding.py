@@ -54,3 +54,36 @@ def test_a_context_is_created_on_its_streams_device(monkeypatch):
         assert seen[-1] == c.device == torch.device(name)
         c.close()
     assert current[0] == torch.device("cuda:0")
+
+
+def test_gradients_are_not_lost_silently(ctx):
+    """The calls record no graph: tensors that require grad are refused while torch records one, and taken under
+    no_grad and in an autograd.Function (where the call reaches the C ABI)."""
+    q, k, cu = heads()
+    z, y, one = torch.zeros((4, 50)), torch.zeros(4, dtype=torch.int64), torch.ones(4)
+    i8, s = torch.zeros((4, 16), dtype=torch.int8), rq.TokenLogprobs(one, one, None, None, None)
+    lse = torch.zeros((4, 6))
+
+    def grad(t):
+        return t.clone().requires_grad_()
+
+    calls = [lambda g: rq.token_logprobs(ctx, g(z), y),
+             lambda g: rq.token_logprobs_backward(ctx, z, y, s, dlogp=g(one)),
+             lambda g: rq.packed_attention(ctx, g(q), k, k, cu),
+             lambda g: rq.packed_attention(ctx, q, k, g(k), cu),
+             lambda g: rq.packed_attention_backward(ctx, q, k, k, cu, g(q), lse, q),
+             lambda g: rq.quantize_rows_i8(ctx, g(z)),
+             lambda g: rq.linear_i8(ctx, i8, one, i8, g(one))]
+
+    class Function(torch.autograd.Function):
+        @staticmethod
+        def forward(c, t, call):
+            call(lambda x: t)
+
+    for call in calls:
+        with pytest.raises(ValueError, match="requires grad"):
+            call(grad)
+        with pytest.raises(AssertionError, match="the C ABI was called"), torch.no_grad():
+            call(grad)
+    with pytest.raises(AssertionError, match="the C ABI was called"):
+        Function.apply(grad(z), calls[0])
