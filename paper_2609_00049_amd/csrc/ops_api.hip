@@ -46,15 +46,22 @@ int guarded(realq_ctx* ctx, F&& body) {
     }
 }
 
+// What a workspace goes by.
+int check_logprobs_sizes(realq_ctx* ctx, const realq_logprobs_desc* d, const std::string& w) {
+    if (d->dtype != REALQ_BF16 && d->dtype != REALQ_F32)
+        return set_error(ctx, REALQ_ERR_INVALID_ARG, w + "dtype must be REALQ_BF16 or REALQ_F32");
+    if (d->T < 0 || d->T > kMostRows || d->V < 1 || d->V > kMostColumns)
+        return set_error(ctx, REALQ_ERR_SHAPE, w + "need 0 <= T, 1 <= V < 2^31");
+    if (d->top < 0 || d->top > REALQ_LOGPROBS_MAX_TOP || d->top > d->V)
+        return set_error(ctx, REALQ_ERR_SHAPE, w + "top must be 0 .. min(V, 64)");
+    return REALQ_OK;
+}
+
 int check_logprobs(realq_ctx* ctx, const realq_logprobs_desc* d, const char* who) {
     const std::string w = std::string(who) + ": ";
     if (!d) return set_error(ctx, REALQ_ERR_INVALID_ARG, w + "NULL descriptor");
-    if (d->dtype != REALQ_BF16 && d->dtype != REALQ_F32)
-        return set_error(ctx, REALQ_ERR_INVALID_ARG, w + "dtype must be REALQ_BF16 or REALQ_F32");
-    if (d->T < 0 || d->T > kMostRows || d->V < 1 || d->V > kMostColumns || d->ld < d->V || d->ld > kMostRows)
-        return set_error(ctx, REALQ_ERR_SHAPE, w + "need 0 <= T, 1 <= V < 2^31, ld >= V");
-    if (d->top < 0 || d->top > REALQ_LOGPROBS_MAX_TOP || d->top > d->V)
-        return set_error(ctx, REALQ_ERR_SHAPE, w + "top must be 0 .. min(V, 64)");
+    if (const int rc = check_logprobs_sizes(ctx, d, w)) return rc;
+    if (d->ld < d->V || d->ld > kMostRows) return set_error(ctx, REALQ_ERR_SHAPE, w + "need ld >= V");
     if (d->T == 0) return REALQ_OK;
     if (!d->logits) return set_error(ctx, REALQ_ERR_INVALID_ARG, w + "NULL logits");
     if (!aligned(d->logits, d->dtype == REALQ_F32 ? 4 : 2) || !aligned(d->targets, 8))
@@ -117,6 +124,7 @@ int realq_token_logprobs_workspace(realq_ctx* ctx, const realq_logprobs_desc* d,
         if (!bytes) return set_error(ctx, REALQ_ERR_INVALID_ARG, "token_logprobs_workspace: NULL bytes");
         if (!d || d->T < 0 || d->V < 1 || d->top < 0)
             return set_error(ctx, REALQ_ERR_INVALID_ARG, "token_logprobs_workspace: bad descriptor");
+        if (const int rc = check_logprobs_sizes(ctx, d, "token_logprobs_workspace: ")) return rc;
         *bytes = realq::logprobs_workspace(d->T, d->V, d->top, d->dtype == REALQ_F32, ctx->cus);
         return REALQ_OK;
     });
