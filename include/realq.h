@@ -559,7 +559,8 @@ int realq_decoder_forward(realq_ctx* ctx, const realq_decoder_desc* desc, realq_
  *              logits (-0 equals 0) by the lower column            [T, top], required when top > 0
  * Masked tokens carry -infinity (p = 0; as alternatives they come last, with log probability
  * -infinity).  A row with nothing but -infinity has lse and log probabilities -infinity and
- * entropy 0.  A row with a NaN or +infinity has NaN results (its top_ids stay in 0 .. V-1).  A
+ * entropy 0.  (Where fewer tokens than `top` are unmasked, or many logits are equal, the row is read once per
+ * alternative.)  A row with a NaN or +infinity has NaN results (its top_ids stay in 0 .. V-1).  A
  * target below 0 stands for no token: logp is 0.  A target of V or more reads nothing: logp is NaN.
  * 1 <= V < 2^31, 0 <= top <= min(V, REALQ_LOGPROBS_MAX_TOP); T == 0 is a no-op.  work: scratch
  * memory of at least realq_token_logprobs_workspace bytes, aligned to 16 (NULL when that is 0);

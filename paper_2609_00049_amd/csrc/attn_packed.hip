@@ -285,9 +285,9 @@ __device__ __forceinline__ Seq ranked_tile(const int32_t* __restrict__ cu, int64
 // maximum, sum and rescaling are the lane's own; only the maximum and the final sum cross to lane + 32.
 // O and the sum are rescaled only when some maximum of the wave has grown by more than 2^8: until then the
 // old one serves as well (P up to 256, exact to the same relative rounding).
-// Bound: the matrix unit beside the exponentials, with 2 waves a SIMD to fill either, at the clock that the board's
-// power leaves (8192 tokens, 32/8 heads x 128: 522 us, 1.05 PFLOP/s, MFMA busy 54% at 1.67 GHz; 4 x 2048: 160 us,
-// 0.86); few tiles: the longest block.
+// Bound: fragments from LDS, each of which feeds one product (a wave holds 32 queries), and the exponentials, with 2
+// waves a SIMD to fill the matrix unit (8192 tokens, 32/8 heads x 128: 522 - 540 us, 1.05 PFLOP/s, MFMA busy 53% at
+// 1.67 GHz; 4 x 2048: 162 us, 0.86); few tiles: the longest block.
 template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) void attn_forward_kernel(AttnArgs a,
                                                                                        uint16_t* __restrict__ O,
@@ -431,8 +431,8 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 64 ? 4 : HD <= 128 ? 2 : 1) voi
 // the rounding of dS to bf16 may move) form dQ once more with the true delta.  Without that, rows with a sink of P
 // near 1 were off by more than their own size (600 tokens x 64 channels); with it by 0.01 of it at most.  The first
 // tile of a sequence, whose rows see few keys, forms delta as sum P dP in a pass of its own before.  Bound: as the
-// forward (8192 tokens, 32/8 heads x 128: 772 us, 1.07 PFLOP/s of its 6 hd operations a pair; 1394 us where every
-// wave takes the second pass).
+// forward (8192 tokens, 32/8 heads x 128: 772 - 790 us, 1.07 PFLOP/s of its 6 hd operations a pair, MFMA busy 60%;
+// 1394 us where every wave takes the second pass).
 template <int HD, int HC, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kernel(
     AttnArgs a, const uint16_t* __restrict__ O, int64_t ldo, const float* __restrict__ lse,
@@ -608,8 +608,8 @@ __global__ __launch_bounds__(256 * GROUPS, HD <= 128 ? 2 : 1) void attn_dq_kerne
 // a block takes one of that many shares of its tile's rounds and leaves float32 sums in `part`
 // ([split][dK, dV][T][n_kv hd]), which sum_splits_kernel adds in their order.  S and dP are formed again, from what
 // the dQ kernel formed too: the one launch that forms them once would add dQ by atomics, in no fixed order.  Bound:
-// LDS reads and the matrix unit in turn (8192 tokens, 32/8 heads x 128: 1085 us, 1.01 PFLOP/s of its 8 hd operations
-// a pair, MFMA busy 49% at 1.81 GHz).
+// LDS reads, three fragments for two products where K and V come from LDS too (8192 tokens, 32/8 heads x 128: 1085 -
+// 1117 us, 1.0 PFLOP/s of its 8 hd operations a pair, MFMA busy 49% at 1.67 - 1.81 GHz).
 template <int HD, int HC, int GROUPS, bool KL, bool DK, bool DV>
 __global__ __launch_bounds__(256 * GROUPS, GROUPS) void attn_dkv_kernel(
     AttnArgs a, const float* __restrict__ lse, const uint16_t* __restrict__ dO, int64_t lddo,
